@@ -397,6 +397,81 @@ rola_status rola_lowrank_readout_combine(const rola_problem* p, const void* Qn, 
                                          const void* Os, const float* gate_logits, float eps,
                                          void* O, hipStream_t stream);
 
+/* ---- around the module: norms, and attention over another set of tokens ------------------------
+ * The other operators of the block that the module sits in (Algorithm "RoLA attention forward pass",
+ * norm_q / norm_k; the block's modulated layer norms and its text cross-attention), with their
+ * gradients. Tensors are taken in place by strides (in elements): 16-byte aligned, every stride of a
+ * dimension longer than one a multiple of 16 bytes, the channels consecutive. Inputs may be
+ * broadcast (stride 0); outputs must not overlap themselves, each other or an input, but may lie between
+ * an input's rows (the parts of one packed tensor). */
+
+/* Layer norm (kind 0) or RMS norm (kind 1) of rows of d channels: xh = (x - mu) rstd with
+ * rstd = (mean (x - mu)^2 + eps)^(-1/2), RMS: mu = 0; y = xh W + Bias. W and Bias are [groups, d], one
+ * row for each rows / groups consecutive rows of X (groups = 1: shared by all); either may be NULL (ones,
+ * zeros). X, Y, dY, dX in dtype with their row strides; W, Bias in wdtype (fp32, or bf16 with a bf16 X).
+ * d a multiple of 8, at most 16384 (ROLA_ERR_UNSUPPORTED beyond), groups at most 65535. */
+typedef enum rola_norm_kind { ROLA_NORM_LAYER = 0, ROLA_NORM_RMS = 1 } rola_norm_kind;
+typedef struct rola_norm_problem {
+  int32_t rows, d, groups;
+  int32_t kind;          /* rola_norm_kind */
+  int32_t dtype, wdtype; /* rola_dtype */
+} rola_norm_problem;
+
+/* Statistics in fp32, y rounded once. mean and rstd (fp32 [rows], either may be NULL) receive the rows'
+ * mu and rstd for the backward; mean is not written for the RMS norm. */
+rola_status rola_norm(const rola_norm_problem* p, const void* X, int64_t ldx, const void* W,
+                      const void* Bias, float eps, void* Y, int64_t ldy, float* mean, float* rstd,
+                      hipStream_t stream);
+
+size_t rola_norm_backward_workspace_bytes(const rola_norm_problem* p);
+
+/* Gradients of <dY, Y>: with g = dY W, dX = rstd (g - mean g - xh mean(g xh)) (RMS: without mean g),
+ * in dtype; dW = sum over the group's rows of dY xh and dB of dY, fp32 [groups, d], added in a fixed
+ * order. dB may be NULL, dW only together with it. mean, rstd: the forward's (mean is not read for the RMS
+ * norm). */
+rola_status rola_norm_backward(const rola_norm_problem* p, const void* X, int64_t ldx, const void* W,
+                               const float* mean, const float* rstd, const void* dY, int64_t ldy,
+                               void* dX, int64_t lddx, float* dW, float* dB, void* ws, size_t ws_bytes,
+                               hipStream_t stream);
+
+/* Softmax attention of Nq queries over Nk keys: O = softmax(scale Q K^T) V over the keys a query sees.
+ * Q, O: [B, H, Nq, d_h]; K, V: [B, Hkv, Nk, d_h], H a multiple of Hkv; query head h reads key head
+ * h / (H / Hkv). Sample b has n = kv_len[b] keys (int32 [B], taken into [0, Nk]; NULL: all Nk); with
+ * causal, query i sees keys j <= i + n - Nq (the last query sees all n). A query that sees no key has
+ * O = 0 and lse = -inf. What lies behind a sample's keys is never used, whatever it holds; a key that the
+ * causal mask hides from a query must still be finite. lse (fp32 [B, H, Nq], may be NULL for the forward) is
+ * log2 of the softmax denominator of the log2e-scaled scores: P = exp2(S log2e - lse), S = scale Q K^T, as
+ * in rola_sparse_attn_lse.
+ * Built for bf16 with d_h = 128 and fp32 with d_h 64 or 128; B H Nq, B Hkv Nk below 2^31, the stride
+ * of the tokens below 2^26 bytes. */
+typedef struct rola_attn_problem {
+  int32_t B, H, Hkv, Nq, Nk, d_h;
+  int32_t dtype;  /* rola_dtype */
+  int32_t causal; /* 0 or 1 */
+} rola_attn_problem;
+/* A [B, heads, N, d_h] tensor in place: element (b, h, n, c) at data[b b + h h + n n + c]. */
+typedef struct rola_heads {
+  void* data;
+  int64_t b, h, n;
+} rola_heads;
+
+/* Workspace of rola_attn: partial results when few rows are split over the keys, else 0 (ws may then be
+ * NULL). */
+size_t rola_attn_workspace_bytes(const rola_attn_problem* p);
+rola_status rola_attn(const rola_attn_problem* p, const rola_heads* Q, const rola_heads* K,
+                      const rola_heads* V, const int32_t* kv_len, float softmax_scale,
+                      const rola_heads* O, float* lse, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Gradients of <dO, O> from O and lse of the forward (same kv_len, scale and mask), the probabilities
+ * recomputed: dQ, dK, dV in dtype, summed in fp32 in a fixed order and rounded once. Keys behind a sample's
+ * last get zero; key heads shared by several query heads get the sum over them. */
+size_t rola_attn_backward_workspace_bytes(const rola_attn_problem* p);
+rola_status rola_attn_backward(const rola_attn_problem* p, const rola_heads* Q, const rola_heads* K,
+                               const rola_heads* V, const int32_t* kv_len, float softmax_scale,
+                               const rola_heads* O, const float* lse, const rola_heads* dO,
+                               const rola_heads* dQ, const rola_heads* dK, const rola_heads* dV,
+                               void* ws, size_t ws_bytes, hipStream_t stream);
+
 #ifdef __cplusplus
 } /* extern "C" */
 #endif

@@ -1,0 +1,130 @@
+// What the kernels of the softmax attention over another set of tokens (attn.hip, attn_grad.hip) share.
+//
+// Rows. The G = H / Hkv query heads that share a key head are the rows of one problem: row r = i G + g is query
+// i of head hk G + g, R = Nq G rows per (b, key head). A tile of rows then reads its keys once for all of
+// them (a single token's G heads are one tile), and its queries' positions stay close together, which is
+// what a causal tile's key range goes by.
+// Keys. Row i sees the keys below limit(i): n = kv_len[b] (clamped to [0, Nk]), and with the causal mask at
+// most i + n - Nq + 1 (the last query sees all n keys). A row with limit <= 0 sees none: its output is zero, its
+// log-sum-exp -inf, and it has no part in any gradient.
+#pragma once
+
+#include "common.h"
+#include "launch.h"
+
+namespace rola {
+
+struct View {
+  char* p;
+  long b, h, n;  // byte strides
+};
+
+struct AttnCall {
+  int Hkv, G, Nq, Nk, causal;
+  const int32_t* kv_len;
+  float scale, scale_log2;
+  View Q, K, V, O;
+};
+
+__device__ __forceinline__ int attn_keys(const AttnCall& a, int b) {
+  return a.kv_len ? max(0, min(a.kv_len[b], a.Nk)) : a.Nk;
+}
+// Keys that query i sees (may be negative).
+__device__ __forceinline__ int attn_limit(const AttnCall& a, int n, int i) {
+  return a.causal ? min(n, i + n - a.Nq + 1) : n;
+}
+
+inline View view_of(const HeadView& v, bool bf) {
+  const long e = bf ? 2 : 4;
+  return View{(char*)const_cast<void*>(v.p), v.b * e, v.h * e, v.n * e};
+}
+inline AttnCall attn_call(const AttnShape& s, const HeadView& Q, const HeadView& K, const HeadView& V,
+                          const HeadView& O, const int32_t* kv_len, float scale) {
+  return AttnCall{s.Hkv, s.H / s.Hkv, s.Nq, s.Nk, s.causal, kv_len, scale, scale * 1.4426950408889634f,
+                  view_of(Q, s.bf16), view_of(K, s.bf16), view_of(V, s.bf16), view_of(O, s.bf16)};
+}
+
+__device__ __forceinline__ f32x16 mfma_bf16(const bf16x8& a, const bf16x8& b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma_f32(float a, float b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+}
+
+// s_waitcnt vmcnt(N), the other counters free.
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
+}
+
+// Sum of x over the lanes l and l ^ 32.
+__device__ __forceinline__ float halves_sum(float x) {
+  const auto v = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(v[0]) + __uint_as_float(v[1]);
+}
+__device__ __forceinline__ float halves_max(float x) {
+  const auto v = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(v[0]), __uint_as_float(v[1]));
+}
+
+// Reference max of a row that has seen no key yet: below every finite score, and finite, so that a hidden
+// key's exp2(-inf - m) is zero and not NaN.
+constexpr float kNoMax = -3e38f;
+
+// ---- fp32 tiles -------------------------------------------------------------------------------------
+// On v_mfma_f32_16x16x4_f32 (A: row l%16, k = l/16; B: column l%16, k = l/16; D: column l%16, rows
+// 4(l/16) + i) with 16-row tiles in LDS, rows padded to D + 4 floats:
+//   f32_rows   X Y^T, X the tile, Y a row per lane in registers; step s of lane group g contracts channel
+//              g D/4 + s, so that both sides are read as 16-byte pieces;
+//   f32_cols   acc += X^T p, p[i] the value of tile row 4g + i (where f32_rows leaves it); row l%16 of channel
+//              tile w is channel (l%16) D/16 + w, again whole pieces.
+template <int D>
+__device__ __forceinline__ f32x4 f32_rows(const float* tile, const float4 (&y)[D / 16], int lane) {
+  const float* row = tile + (lane % 16) * (D + 4) + (lane / 16) * (D / 4);
+  f32x4 s0 = f32x4{0.f, 0.f, 0.f, 0.f}, s1 = s0;
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) {
+    const float4 x = *reinterpret_cast<const float4*>(row + 4 * s);
+    s0 = mfma_f32(x.x, y[s].x, s0);
+    s1 = mfma_f32(x.y, y[s].y, s1);
+    s0 = mfma_f32(x.z, y[s].z, s0);
+    s1 = mfma_f32(x.w, y[s].w, s1);
+  }
+  return s0 + s1;
+}
+template <int D>
+__device__ __forceinline__ void f32_cols(const float* tile, const float (&p)[4], f32x4 (&acc)[D / 16],
+                                         int lane) {
+  constexpr int W = D / 16;
+  const float* at = tile + 4 * (lane / 16) * (D + 4) + (lane % 16) * W;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int s = 0; s < W / 4; ++s) {
+      const float4 x = *reinterpret_cast<const float4*>(at + i * (D + 4) + 4 * s);
+      acc[4 * s] = mfma_f32(x.x, p[i], acc[4 * s]);
+      acc[4 * s + 1] = mfma_f32(x.y, p[i], acc[4 * s + 1]);
+      acc[4 * s + 2] = mfma_f32(x.z, p[i], acc[4 * s + 2]);
+      acc[4 * s + 3] = mfma_f32(x.w, p[i], acc[4 * s + 3]);
+    }
+}
+// A lane's quarter of a row, for f32_rows.
+template <int D>
+__device__ __forceinline__ void f32_quarter(const char* row, int lane, float4 (&y)[D / 16]) {
+  const float4* at = reinterpret_cast<const float4*>(row) + (lane / 16) * (D / 16);
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) y[s] = at[s];
+}
+// Stores a row from f32_cols' accumulators (lane: row l%16, channels (4g + i) W + w), scaled by f.
+template <int D>
+__device__ __forceinline__ void f32_store(char* row, const f32x4 (&acc)[D / 16], float f, int lane) {
+  constexpr int W = D / 16;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int s = 0; s < W / 4; ++s)
+      reinterpret_cast<float4*>(row)[((4 * (lane / 16) + i) * W) / 4 + s] =
+          make_float4(acc[4 * s][i] * f, acc[4 * s + 1][i] * f, acc[4 * s + 2][i] * f, acc[4 * s + 3][i] * f);
+}
+
+}  // namespace rola

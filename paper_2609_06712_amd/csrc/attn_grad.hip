@@ -1,0 +1,713 @@
+// Gradients of the softmax attention of attn.hip (attn_common.h): from dO, O and the forward's log-sum-exp,
+//   P = exp2(S scale log2e - lse),  D = rowsum(dO O),  dP = dO V^T,  dS = P (dP - D),
+//   dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO  (dK, dV summed over the query heads of a key head).
+// The probabilities are recomputed, twice, so that every gradient is summed in registers in a fixed order
+// and is rounded once: a pass over the keys per tile of rows (dQ, three products) and a pass over the queries
+// per block of keys (dK, dV, four). Bound by the matrix cores (14 d operations per visible pair against the ten
+// of a single pass, which would have to add dQ in memory).
+//
+// Row statistics: attn_rowdot_kernel packs {lse, D} per query, per head padded to whole tiles of 32 with
+// {inf, 0}: P is then zero for rows past the last and for rows that see no key, with no test in the walk.
+//
+// When a pass has too few workgroups for the chip, each tile's walk is cut into parts whose fp32 sums go to the
+// workspace and are added in order by attn_sum_kernel.
+#include <algorithm>
+
+#include "attn_common.h"
+
+namespace rola {
+namespace {
+
+constexpr int kRows = 32;            // rows of a sub-tile
+constexpr int kTile = kRows * 256;   // its bytes (bf16, d 128)
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+struct GradArgs {
+  AttnCall c;     // c.O: dO
+  View G1, G2;    // dQ; or dK, dV
+  int tiles, splits, total, R, Np;
+  const float2* lseD;  // [B, H, Np]
+  float* part;         // splits > 1: [B Hkv][splits][rows][d], dV's after dK's
+  long part2;          // elements between dK's and dV's partials
+};
+
+__global__ __launch_bounds__(256) void attn_rowdot_bf16_kernel(int H, int Nq, int Np, long rows, View O, View dO,
+                                                               const float* __restrict__ lse,
+                                                               float2* __restrict__ lseD) {
+  const long row = ((long)blockIdx.x * 256 + threadIdx.x) / 16;  // (b, h, padded query)
+  const int part = threadIdx.x % 16;
+  if (row >= rows) return;
+  const long bh = row / Np;
+  const int i = (int)(row % Np), b = (int)(bh / H), h = (int)(bh % H);
+  float s = 0.f;
+  if (i < Nq) {
+    float x[8], y[8];
+    load8(reinterpret_cast<const bf16*>(O.p + b * O.b + h * O.h + i * O.n) + part * 8, x);
+    load8(reinterpret_cast<const bf16*>(dO.p + b * dO.b + h * dO.h + i * dO.n) + part * 8, y);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s = fmaf(x[k], y[k], s);
+  }
+#pragma unroll
+  for (int off = 8; off >= 1; off >>= 1) s += __shfl_xor(s, off, 16);
+  if (part == 0) {
+    const float l = i < Nq ? lse[bh * Nq + i] : -__builtin_inff();
+    const bool none = l == -__builtin_inff();
+    lseD[row] = make_float2(none ? __builtin_inff() : l, none ? 0.f : s);
+  }
+}
+
+__global__ __launch_bounds__(256) void attn_rowdot_f32_kernel(int H, int Nq, int Np, int d, long rows, View O,
+                                                              View dO, const float* __restrict__ lse,
+                                                              float2* __restrict__ lseD) {
+  const long row = ((long)blockIdx.x * 256 + threadIdx.x) / 16;
+  const int part = threadIdx.x % 16;
+  if (row >= rows) return;
+  const long bh = row / Np;
+  const int i = (int)(row % Np), b = (int)(bh / H), h = (int)(bh % H);
+  float s = 0.f;
+  if (i < Nq) {
+    const float4* x = reinterpret_cast<const float4*>(O.p + b * O.b + h * O.h + i * O.n);
+    const float4* y = reinterpret_cast<const float4*>(dO.p + b * dO.b + h * dO.h + i * dO.n);
+    for (int e = part; e < d / 4; e += 16) {
+      const float4 u = x[e], v = y[e];
+      s = fmaf(u.x, v.x, fmaf(u.y, v.y, fmaf(u.z, v.z, fmaf(u.w, v.w, s))));
+    }
+  }
+#pragma unroll
+  for (int off = 8; off >= 1; off >>= 1) s += __shfl_xor(s, off, 16);
+  if (part == 0) {
+    const float l = i < Nq ? lse[bh * Nq + i] : -__builtin_inff();
+    const bool none = l == -__builtin_inff();
+    lseD[row] = make_float2(none ? __builtin_inff() : l, none ? 0.f : s);
+  }
+}
+
+// ---- dQ ------------------------------------------------------------------------------------------------
+
+struct Part {
+  int tile, split, b, hk;
+  long bh;
+};
+__device__ __forceinline__ Part part_of(const GradArgs& a, int L, bool longest_last) {
+  Part p;
+  const int t = L % a.tiles, rest = L / a.tiles;
+  p.tile = longest_last ? a.tiles - 1 - t : t;
+  p.split = rest % a.splits;
+  p.bh = rest / a.splits;
+  p.b = (int)(p.bh / a.c.Hkv);
+  p.hk = (int)(p.bh % a.c.Hkv);
+  return p;
+}
+
+// Stores 128 channels of a row from the accumulator layout of a 32x32 tile set, rounded to bf16.
+__device__ __forceinline__ void store_row_bf16(char* row, const f32x16 (&acc)[4], float f, int hh) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      bf16x4 o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = (bf16)(acc[w][4 * j + e] * f);
+      *reinterpret_cast<bf16x4*>(row + 2 * (32 * w + 8 * j + 4 * hh)) = o;
+    }
+}
+
+// Four waves of 32 rows walk the keys in sub-tiles of 32 through three LDS stages:
+//   S^T = K Q^T, dP^T = V dO^T (a lane has one row and 16 keys of it), dQ^T += K^T dS^T.
+__global__ __launch_bounds__(256, 2) void attn_dq_bf16_kernel(const GradArgs a) {
+  constexpr int STAGE = 2 * kTile, NBUF = 3, DPW = 2;
+  __shared__ __attribute__((aligned(1024))) char lds[NBUF * STAGE];
+  const AttnCall& c = a.c;
+  const Part pt = part_of(a, xcd_remap(blockIdx.x, a.total), c.causal);
+  const int wave = wave_uniform(threadIdx.x / 64), lane = threadIdx.x % 64, hh = lane / 32;
+  const int n = attn_keys(c, pt.b);
+  const int row0 = (pt.tile * 4 + wave) * 32;
+  const int r = min(row0 + lane % 32, a.R - 1), i = r / c.G, head = pt.hk * c.G + r % c.G;
+  const int lim = attn_limit(c, n, i);
+  const int lim_lo = attn_limit(c, n, min(row0, a.R - 1) / c.G);
+  const int lim_hi = row0 < a.R ? attn_limit(c, n, min(row0 + 31, a.R - 1) / c.G) : 0;
+  const int end = max(0, attn_limit(c, n, min(pt.tile * 128 + 127, a.R - 1) / c.G));
+  const int all = (end + 31) / 32, per = (all + a.splits - 1) / a.splits;
+  const int first = pt.split * per, T = max(0, min(all, first + per) - first);
+  const char* Kh = c.K.p + pt.b * c.K.b + pt.hk * c.K.h;
+  const char* Vh = c.V.p + pt.b * c.V.b + pt.hk * c.V.h;
+  uint32_t dk[DPW], dv[DPW];
+#pragma unroll
+  for (int x = 0; x < DPW; ++x) {
+    const int row = 4 * (wave * DPW + x) + lane / 16;
+    const uint32_t chunk = ((lane % 16) ^ bw_swizzle(row)) << 4;
+    dk[x] = row * (uint32_t)c.K.n + chunk;
+    dv[x] = row * (uint32_t)c.V.n + chunk;
+  }
+  const uint32_t lds0 = lds_address(lds) + wave * DPW * 1024;
+  bf16x8 qf[8], df[8];
+  {
+    const char* q = c.Q.p + pt.b * c.Q.b + head * c.Q.h + i * c.Q.n + 16 * hh;
+    const char* o = c.O.p + pt.b * c.O.b + head * c.O.h + i * c.O.n + 16 * hh;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      qf[s] = *reinterpret_cast<const bf16x8*>(q + 32 * s);
+      df[s] = *reinterpret_cast<const bf16x8*>(o + 32 * s);
+    }
+  }
+  const float2 ld = a.lseD[((long)pt.b * c.Hkv * c.G + head) * a.Np + i];
+  wait_vm<0>();
+  f32x16 acc[4];
+#pragma unroll
+  for (int w = 0; w < 4; ++w) acc[w] = f32x16{};
+
+  auto issue = [&](int t, int buf) {
+    const int k0 = (first + t) * 32;
+    const uint32_t dst = lds0 + buf * STAGE;
+    const char* kb = Kh + (long)k0 * c.K.n;
+    const char* vb = Vh + (long)k0 * c.V.n;
+#pragma unroll
+    for (int x = 0; x < DPW; ++x) {
+      uint32_t ok = dk[x], ov = dv[x];
+      if (k0 + 32 > n) {  // rows past the last key re-read it
+        const int back = max(4 * (wave * DPW + x) + lane / 16 - (n - 1 - k0), 0);
+        ok -= back * (uint32_t)c.K.n;
+        ov -= back * (uint32_t)c.V.n;
+      }
+      dma16(kb, ok, dst + x * 1024);
+      dma16(vb, ov, dst + kTile + x * 1024);
+    }
+  };
+  int issued = 0;
+#pragma unroll
+  for (int j = 0; j < NBUF - 1; ++j)
+    if (j < T) issue(j, j), ++issued;
+  for (int t = 0; t < T;) {
+#pragma unroll
+    for (int j = 0; j < NBUF; ++j) {
+      if (t >= T) break;
+      if (issued == t + NBUF - 1)
+        wait_vm<2 * DPW * (NBUF - 2)>();
+      else
+        __builtin_amdgcn_s_waitcnt(0);
+      __syncthreads();
+      if (issued < T) issue(issued, (j + NBUF - 1) % NBUF), ++issued;
+      const int k0 = (first + t) * 32;
+      if (k0 < lim_hi) {
+        const char* Kt = lds + j * STAGE;
+        const char* Vt = Kt + kTile;
+        bf16x8 ka[8], va[8], kt[8];
+        f32x16 sc = f32x16{}, dp = f32x16{};
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+          ka[s] = row_frag(Kt, lane % 32, s, hh);
+          va[s] = row_frag(Vt, lane % 32, s, hh);
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int w = 0; w < 4; ++w) kt[4 * u + w] = tr_frag(Kt, w, u, lane);
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+          sc = mfma_bf16(ka[s], qf[s], sc);
+          dp = mfma_bf16(va[s], df[s], dp);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);  // DS reads
+#pragma unroll
+        for (int s = 0; s < 16; ++s) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // MFMA
+          __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        }
+        if (k0 + 32 > lim_lo) {  // value k: key k0 + 8(k/4) + 4 hh + k%4 of this lane's row
+          const int left = lim - k0 - 4 * hh;
+#pragma unroll
+          for (int k = 0; k < 16; ++k) sc[k] = 8 * (k / 4) + k % 4 < left ? sc[k] : -__builtin_inff();
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        bf16x8 ds[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float p = __builtin_amdgcn_exp2f(fmaf(sc[8 * u + k], c.scale_log2, -ld.x));
+            ds[u][k] = (bf16)(p * (dp[8 * u + k] - ld.y));
+          }
+#pragma unroll
+          for (int w = 0; w < 4; ++w) acc[w] = mfma_bf16(kt[4 * u + w], ds[u], acc[w]);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x402, 36, 0);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x402, 9, 0);
+        }
+      }
+      ++t;
+    }
+  }
+  if (row0 + lane % 32 >= a.R) return;
+  if (a.splits > 1)
+    store_grad_row<false>(a.part + ((pt.bh * a.splits + pt.split) * a.R + r) * 128, acc, c.scale, hh, nullptr,
+                          nullptr);
+  else
+    store_row_bf16(a.G1.p + pt.b * a.G1.b + head * a.G1.h + i * a.G1.n, acc, c.scale, hh);
+}
+
+// fp32: four waves of 16 rows, key tiles of 32 staged in LDS.
+template <int D>
+__global__ __launch_bounds__(256) void attn_dq_f32_kernel(const GradArgs a) {
+  constexpr int W = D / 16, LD = D + 4, PT = 32 * D / 4 / 256;
+  __shared__ __attribute__((aligned(16))) float ks[32 * LD], vs[32 * LD];
+  const AttnCall& c = a.c;
+  const Part pt = part_of(a, xcd_remap(blockIdx.x, a.total), c.causal);
+  const int wave = wave_uniform(threadIdx.x / 64), lane = threadIdx.x % 64, gr = lane / 16;
+  const int n = attn_keys(c, pt.b);
+  const int row0 = pt.tile * 64 + wave * 16;
+  const int r = min(row0 + lane % 16, a.R - 1), i = r / c.G, head = pt.hk * c.G + r % c.G;
+  const int lim = attn_limit(c, n, i);
+  const int lim_hi = row0 < a.R ? attn_limit(c, n, min(row0 + 15, a.R - 1) / c.G) : 0;
+  const int end = max(0, attn_limit(c, n, min(pt.tile * 64 + 63, a.R - 1) / c.G));
+  const int all = (end + 31) / 32, per = (all + a.splits - 1) / a.splits;
+  const int t0 = pt.split * per, t1 = min(all, t0 + per);
+  const char* Kh = c.K.p + pt.b * c.K.b + pt.hk * c.K.h;
+  const char* Vh = c.V.p + pt.b * c.V.b + pt.hk * c.V.h;
+  float4 qv[W], dv[W];
+  f32_quarter<D>(c.Q.p + pt.b * c.Q.b + head * c.Q.h + i * c.Q.n, lane, qv);
+  f32_quarter<D>(c.O.p + pt.b * c.O.b + head * c.O.h + i * c.O.n, lane, dv);
+  const float2 ld = a.lseD[((long)pt.b * c.Hkv * c.G + head) * a.Np + i];
+  f32x4 acc[W];
+#pragma unroll
+  for (int w = 0; w < W; ++w) acc[w] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float4 kn[PT], vn[PT];
+  auto fetch = [&](int t) {
+#pragma unroll
+    for (int x = 0; x < PT; ++x) {
+      const int e = threadIdx.x + 256 * x, row = e / (D / 4), at = e % (D / 4);
+      const long key = min(t * 32 + row, n - 1);
+      kn[x] = reinterpret_cast<const float4*>(Kh + key * c.K.n)[at];
+      vn[x] = reinterpret_cast<const float4*>(Vh + key * c.V.n)[at];
+    }
+  };
+  if (t0 < t1) fetch(t0);
+  for (int t = t0; t < t1; ++t) {
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < PT; ++x) {
+      const int e = threadIdx.x + 256 * x, row = e / (D / 4), at = e % (D / 4);
+      *reinterpret_cast<float4*>(ks + row * LD + 4 * at) = kn[x];
+      *reinterpret_cast<float4*>(vs + row * LD + 4 * at) = vn[x];
+    }
+    __syncthreads();
+    if (t + 1 < t1) fetch(t + 1);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int k0 = t * 32 + 16 * u;
+      if (k0 >= lim_hi) break;
+      const f32x4 sc = f32_rows<D>(ks + 16 * u * LD, qv, lane);
+      const f32x4 dp = f32_rows<D>(vs + 16 * u * LD, dv, lane);
+      float ds[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float p = k0 + 4 * gr + k < lim ? __builtin_amdgcn_exp2f(fmaf(sc[k], c.scale_log2, -ld.x)) : 0.f;
+        ds[k] = p * (dp[k] - ld.y);
+      }
+      f32_cols<D>(ks + 16 * u * LD, ds, acc, lane);
+    }
+  }
+  if (row0 + lane % 16 >= a.R) return;
+  char* out = a.splits > 1
+                  ? reinterpret_cast<char*>(a.part + ((pt.bh * a.splits + pt.split) * a.R + r) * D)
+                  : a.G1.p + pt.b * a.G1.b + head * a.G1.h + i * a.G1.n;
+  f32_store<D>(out, acc, c.scale, lane);
+}
+
+// ---- dK, dV ----------------------------------------------------------------------------------------------
+
+// The walk of a block of keys: steps of 32 queries, the query heads of its key head one after the other, each from
+// the first tile of queries that can see the block.
+struct Walk {
+  int q0, tiles, t0, t1;  // first query (a multiple of 32), tiles per head, steps of this part
+};
+__device__ __forceinline__ Walk walk_of(const GradArgs& a, int n, int key0, int split) {
+  const AttnCall& c = a.c;
+  Walk w;
+  w.q0 = c.causal ? max(0, key0 - (n - c.Nq)) / 32 * 32 : 0;
+  w.tiles = key0 < n && w.q0 < c.Nq ? (c.Nq - w.q0 + 31) / 32 : 0;
+  const int all = w.tiles * c.G, per = (all + a.splits - 1) / a.splits;
+  w.t0 = split * per;
+  w.t1 = max(w.t0, min(all, w.t0 + per));
+  return w;
+}
+
+// bf16: a workgroup has 128 keys, in two roles of four waves over the same 32-key columns. Role 0 holds the
+// keys' K: S = Q K^T, P, dV^T += dO^T P. Role 1 holds their V: dP = dO V^T, dS = P (dP - D), dK^T += Q^T dS, with
+// P from role 0 through LDS one step later, as fp16 (P lies in [0, 1], where that is an eighth of the
+// rounding to bf16 that dS takes next). A wave then has one operand set and one accumulator set, and two waves
+// run per SIMD. Operands are read from LDS a product ahead: the next step's rows during the second product,
+// the transposed ones during the first.
+constexpr int kDkvBuf = 4;
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void attn_dkv_bf16_kernel(const GradArgs a) {
+  constexpr int NKW = 4, STAGE = 2 * kTile + 1024, DPW = 2, PBUF = NKW * 2048, NBUF = kDkvBuf;
+  constexpr int AHEAD = NBUF - 3;
+  static_assert(AHEAD == 1, "every load in flight is the next step's: the waits below are for all of them");
+  __shared__ __attribute__((aligned(1024))) char lds[NBUF * STAGE + 2 * PBUF];
+  const AttnCall& c = a.c;
+  const Part pt = part_of(a, xcd_remap(blockIdx.x, a.total), false);
+  const int lane = threadIdx.x % 64, hh = lane / 32;
+  const int wave = wave_uniform(threadIdx.x / 64), role = wave / NKW, kw = wave % NKW;
+  const int n = attn_keys(c, pt.b), off = n - c.Nq;
+  const int key0 = pt.tile * 128, key = key0 + kw * 32 + lane % 32;
+  const Walk wk = walk_of(a, n, key0, pt.split);
+  const int T = wk.t1 - wk.t0;
+
+  bf16x8 bf[8];
+  {
+    const View& src = role ? c.V : c.K;
+    const char* row = src.p + pt.b * src.b + pt.hk * src.h + (long)max(0, min(key, n - 1)) * src.n + 16 * hh;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) bf[s] = *reinterpret_cast<const bf16x8*>(row + 32 * s);
+  }
+  wait_vm<0>();
+  f32x16 acc[4];
+#pragma unroll
+  for (int w = 0; w < 4; ++w) acc[w] = f32x16{};
+
+  // Loads of a step: waves 0-3 the Q rows, waves 4-7 the dO rows, 8 rows each.
+  const View& mine = wave < 4 ? c.Q : c.O;
+  uint32_t dsrc[DPW];
+#pragma unroll
+  for (int x = 0; x < DPW; ++x) {
+    const int row = 4 * ((wave % 4) * DPW + x) + lane / 16;
+    dsrc[x] = row * (uint32_t)mine.n + (((lane % 16) ^ bw_swizzle(row)) << 4);
+  }
+  const uint32_t lds0 = lds_address(lds);
+  const uint32_t dst0 = lds0 + (wave / 4) * kTile + (wave % 4) * DPW * 1024;
+  const char* mbase = mine.p + pt.b * mine.b + (long)pt.hk * c.G * mine.h;
+  const char* lbase = reinterpret_cast<const char*>(a.lseD + ((long)pt.b * c.Hkv + pt.hk) * c.G * a.Np);
+  int ig = 0, iq = wk.q0, cq = wk.q0;  // the next step to load; the query of the next step to take
+  if (wk.tiles > 0) {
+    ig = wk.t0 / wk.tiles;
+    iq = cq = wk.q0 + wk.t0 % wk.tiles * 32;
+  }
+  auto issue = [&](int buf) {
+    const char* base = mbase + ig * mine.h + (long)iq * mine.n;
+    const uint32_t dst = dst0 + buf * STAGE;
+#pragma unroll
+    for (int x = 0; x < DPW; ++x) {
+      uint32_t o = dsrc[x];
+      if (iq + 32 > c.Nq)  // rows past the last query re-read it (P = 0 there)
+        o -= max(4 * ((wave % 4) * DPW + x) + lane / 16 - (c.Nq - 1 - iq), 0) * (uint32_t)mine.n;
+      dma16(base, o, dst + x * 1024);
+    }
+    // lse, D of the 32 queries (256 bytes; lanes 16-63 repeat lanes 0-15)
+    if (wave == 0)
+      dma16(lbase + ((long)ig * a.Np + iq) * 8, (lane % 16) * 16, lds0 + buf * STAGE + 2 * kTile);
+    iq += 32;
+    if (iq >= c.Nq) iq = wk.q0, ++ig;
+  };
+
+  char* pbase = lds + NBUF * STAGE + kw * 2048 + lane * 16;  // + buffer * PBUF + u * 1024
+  int issued = 0;
+#pragma unroll
+  for (int j = 0; j <= AHEAD; ++j)
+    if (j < T) issue(j), ++issued;
+  wait_vm<0>();
+  __syncthreads();
+  // Iteration t: role 0 takes step t, role 1 step t - 1. Both meet the same barriers, in whole turns of NBUF.
+  auto walk = [&](auto role_tag) {
+    constexpr int ROLE = decltype(role_tag)::value;
+    bf16x8 fa[8];  // row operands (Q for role 0, dO for role 1) of the wave's next step
+    auto row_operands = [&](int stage) {
+#pragma unroll
+      for (int s = 0; s < 8; ++s) fa[s] = row_frag(lds + stage * STAGE + ROLE * kTile, lane % 32, s, hh);
+    };
+    if (ROLE == 0) row_operands(0);
+    for (int t = 0; t <= T;) {
+#pragma unroll
+      for (int b = 0; b < NBUF; ++b, ++t) {
+        wait_vm<0>();  // stage t + 1 has landed
+        __syncthreads();
+        if (issued < T) issue((b + 1 + AHEAD) % NBUF), ++issued;
+        const int step = t - ROLE;
+        if (step >= 0 && step < T) {
+          const char* stage = lds + (ROLE ? (b + NBUF - 1) % NBUF : b) * STAGE;
+          const float* lt = reinterpret_cast<const float*>(stage + 2 * kTile) + ROLE;
+          char* pb = pbase + ((b + ROLE) % 2) * PBUF;  // role 0 writes step t's, role 1 reads t - 1's
+          bf16x8 fb[8];
+#pragma unroll
+          for (int w = 0; w < 4; ++w)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) fb[2 * w + u] = tr_frag(stage + (1 - ROLE) * kTile, w, u, lane);
+          float lv[16];  // lse (role 0) or D (role 1) of the step's queries
+#pragma unroll
+          for (int k = 0; k < 16; ++k) lv[k] = lt[2 * (8 * (k / 4) + 4 * hh + k % 4)];
+          // S (role 0) or dP (role 1): one lane per key; rows 8j + 4(l/32) + e are the step's queries
+          f32x16 X = f32x16{};
+#pragma unroll
+          for (int s = 0; s < 8; ++s) X = mfma_bf16(fa[s], bf[s], X);
+          f16x8 ph[2];
+          if constexpr (ROLE == 1) {
+            ph[0] = *reinterpret_cast<const f16x8*>(pb);
+            ph[1] = *reinterpret_cast<const f16x8*>(pb + 1024);
+          }
+          __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+#pragma unroll
+          for (int s = 0; s < 8; ++s) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+          row_operands(ROLE ? b : (b + 1) % NBUF);
+          if (ROLE == 0 && c.causal && key0 + 127 > cq + off) {  // P = 0 where the query is before the key
+            const int late = key - off - cq - 4 * hh;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) lv[k] = 8 * (k / 4) + k % 4 >= late ? lv[k] : __builtin_inff();
+          }
+          cq += 32;
+          if (cq >= c.Nq) cq = wk.q0;
+          __builtin_amdgcn_sched_barrier(0);
+          bf16x8 b2[2];
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              if constexpr (ROLE == 0) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(X[8 * u + k], c.scale_log2, -lv[8 * u + k]));
+                b2[u][k] = (bf16)p;
+                ph[u][k] = (_Float16)p;
+              } else {
+                b2[u][k] = (bf16)((float)ph[u][k] * (X[8 * u + k] - lv[8 * u + k]));
+              }
+            }
+            if constexpr (ROLE == 0) *reinterpret_cast<f16x8*>(pb + 1024 * u) = ph[u];
+#pragma unroll
+            for (int w = 0; w < 4; ++w) acc[w] = mfma_bf16(fb[2 * w + u], b2[u], acc[w]);
+          }
+          __builtin_amdgcn_sched_group_barrier(0x402, 28, 0);
+#pragma unroll
+          for (int s = 0; s < 4; ++s) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x402, 7, 0);
+          }
+        } else if (step < 0) {
+          row_operands(0);
+        }
+      }
+    }
+  };
+  if (T > 0) {
+    if (role)
+      walk(std::integral_constant<int, 1>{});
+    else
+      walk(std::integral_constant<int, 0>{});
+  }
+  if (key >= c.Nk) return;
+  if (key >= n) {  // a key that is not there (its column holds the last one's)
+#pragma unroll
+    for (int w = 0; w < 4; ++w) acc[w] = f32x16{};
+  }
+  const float f = role ? c.scale : 1.f;
+  if (a.splits > 1) {
+    float* out = a.part + (role ? 0 : a.part2) + ((pt.bh * a.splits + pt.split) * c.Nk + key) * 128;
+    store_grad_row<false>(out, acc, f, hh, nullptr, nullptr);
+  } else {
+    const View& g = role ? a.G1 : a.G2;
+    store_row_bf16(g.p + pt.b * g.b + pt.hk * g.h + key * g.n, acc, f, hh);
+  }
+}
+
+// fp32: four waves of 16 keys each, query tiles of 32 staged in LDS.
+template <int D>
+__global__ __launch_bounds__(256) void attn_dkv_f32_kernel(const GradArgs a) {
+  constexpr int W = D / 16, LD = D + 4, PT = 32 * D / 4 / 256;
+  __shared__ __attribute__((aligned(16))) float qs[32 * LD], os[32 * LD];
+  __shared__ float2 st[32];
+  const AttnCall& c = a.c;
+  const Part pt = part_of(a, xcd_remap(blockIdx.x, a.total), false);
+  const int wave = wave_uniform(threadIdx.x / 64), lane = threadIdx.x % 64, gr = lane / 16;
+  const int n = attn_keys(c, pt.b), off = n - c.Nq;
+  const int key0 = pt.tile * 64, key = key0 + wave * 16 + lane % 16;
+  const Walk wk = walk_of(a, n, key0, pt.split);
+  float4 kv[W], vv[W];
+  {
+    const long k = max(0, min(key, n - 1));
+    f32_quarter<D>(c.K.p + pt.b * c.K.b + pt.hk * c.K.h + k * c.K.n, lane, kv);
+    f32_quarter<D>(c.V.p + pt.b * c.V.b + pt.hk * c.V.h + k * c.V.n, lane, vv);
+  }
+  f32x4 dk[W], dv[W];
+#pragma unroll
+  for (int w = 0; w < W; ++w) dk[w] = dv[w] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float4 qn[PT], on[PT];
+  float2 sn = make_float2(0.f, 0.f);
+  int g = 0, q = wk.q0;
+  if (wk.tiles > 0) {
+    g = wk.t0 / wk.tiles;
+    q = wk.q0 + wk.t0 % wk.tiles * 32;
+  }
+  auto fetch = [&]() {
+    const int head = pt.hk * c.G + g;
+    const char* Qh = c.Q.p + pt.b * c.Q.b + head * c.Q.h;
+    const char* Oh = c.O.p + pt.b * c.O.b + head * c.O.h;
+#pragma unroll
+    for (int x = 0; x < PT; ++x) {
+      const int e = threadIdx.x + 256 * x, row = e / (D / 4), at = e % (D / 4);
+      const long i = min(q + row, c.Nq - 1);
+      qn[x] = reinterpret_cast<const float4*>(Qh + i * c.Q.n)[at];
+      on[x] = reinterpret_cast<const float4*>(Oh + i * c.O.n)[at];
+    }
+    if (threadIdx.x < 32) sn = a.lseD[((long)pt.b * c.Hkv * c.G + head) * a.Np + q + threadIdx.x];
+  };
+  if (wk.t0 < wk.t1) fetch();
+  for (int t = wk.t0; t < wk.t1; ++t) {
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < PT; ++x) {
+      const int e = threadIdx.x + 256 * x, row = e / (D / 4), at = e % (D / 4);
+      *reinterpret_cast<float4*>(qs + row * LD + 4 * at) = qn[x];
+      *reinterpret_cast<float4*>(os + row * LD + 4 * at) = on[x];
+    }
+    if (threadIdx.x < 32) st[threadIdx.x] = sn;
+    __syncthreads();
+    const int q0 = q;
+    q += 32;
+    if (q >= c.Nq) q = wk.q0, ++g;
+    if (t + 1 < wk.t1) fetch();
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const f32x4 sc = f32_rows<D>(qs + 16 * u * LD, kv, lane);
+      const f32x4 dp = f32_rows<D>(os + 16 * u * LD, vv, lane);
+      float p[4], ds[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {  // query q0 + 16 u + 4 gr + k
+        const int row = 16 * u + 4 * gr + k;
+        const float2 s = st[row];
+        const bool seen = !c.causal || key <= q0 + row + off;
+        p[k] = seen ? __builtin_amdgcn_exp2f(fmaf(sc[k], c.scale_log2, -s.x)) : 0.f;
+        ds[k] = p[k] * (dp[k] - s.y);
+      }
+      f32_cols<D>(os + 16 * u * LD, p, dv, lane);
+      f32_cols<D>(qs + 16 * u * LD, ds, dk, lane);
+    }
+  }
+  if (key >= c.Nk) return;
+  const float live = key < n ? 1.f : 0.f;
+  char *pk, *pv;
+  if (a.splits > 1) {
+    float* out = a.part + ((pt.bh * a.splits + pt.split) * c.Nk + key) * D;
+    pk = reinterpret_cast<char*>(out);
+    pv = reinterpret_cast<char*>(out + a.part2);
+  } else {
+    pk = a.G1.p + pt.b * a.G1.b + pt.hk * a.G1.h + key * a.G1.n;
+    pv = a.G2.p + pt.b * a.G2.b + pt.hk * a.G2.h + key * a.G2.n;
+  }
+  f32_store<D>(pk, dk, c.scale * live, lane);
+  f32_store<D>(pv, dv, live, lane);
+}
+
+// out row = sum of its parts, in order: part [B Hkv][splits][rows][D]; a row r is head hk G + r % G, token
+// r / G. A thread takes four channels.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void attn_sum_kernel(int Hkv, int G, int rows, int splits, long total,
+                                                       const float* __restrict__ part, View out) {
+  const long e = (long)blockIdx.x * 256 + threadIdx.x;
+  const long at = e / (D / 4);
+  const int c = 4 * (int)(e % (D / 4));
+  if (at >= total) return;
+  const long bh = at / rows;
+  const int r = (int)(at % rows);
+  const float* src = part + (bh * splits * rows + r) * D + c;
+  float4 s = *reinterpret_cast<const float4*>(src);
+  for (int k = 1; k < splits; ++k) {
+    const float4 v = *reinterpret_cast<const float4*>(src + (long)k * rows * D);
+    s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+  }
+  const int b = (int)(bh / Hkv), head = (int)(bh % Hkv) * G + r % G;
+  T* o = reinterpret_cast<T*>(out.p + b * out.b + head * out.h + (long)(r / G) * out.n) + c;
+  o[0] = from_f32<T>(s.x), o[1] = from_f32<T>(s.y), o[2] = from_f32<T>(s.z), o[3] = from_f32<T>(s.w);
+}
+
+struct GradPlan {
+  int R, Np;
+  int qtiles, qsplits, ktiles, ksplits;
+  size_t lsed, qpart, kpart;  // bytes, 256-aligned; kpart: of dK, and as many of dV
+};
+size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+GradPlan grad_plan(const AttnShape& s) {
+  GradPlan p;
+  const int G = s.H / s.Hkv;
+  const long bh = (long)s.B * s.Hkv;
+  p.R = s.Nq * G;
+  p.Np = (s.Nq + 31) / 32 * 32;
+  const int qrows = s.bf16 ? 128 : 64, krows = s.bf16 ? 128 : 64;
+  p.qtiles = (p.R + qrows - 1) / qrows;
+  p.ktiles = (s.Nk + krows - 1) / krows;
+  // parts: one round of the workgroups that the chip holds, of at least 256 keys or 512 queries each
+  const long qhold = 2 * kCus, khold = (s.bf16 ? 1 : 2) * kCus;
+  p.qsplits = (int)std::max<long>(1, std::min<long>({qhold / (p.qtiles * bh), (s.Nk + 255) / 256, 64}));
+  p.ksplits = (int)std::max<long>(1, std::min<long>({khold / (p.ktiles * bh), ((long)p.R + 511) / 512, 64}));
+  p.lsed = up256((size_t)s.B * s.H * p.Np * sizeof(float2));
+  p.qpart = p.qsplits > 1 ? up256((size_t)bh * p.qsplits * p.R * s.d * 4) : 0;
+  p.kpart = p.ksplits > 1 ? up256((size_t)bh * p.ksplits * s.Nk * s.d * 4) : 0;
+  return p;
+}
+
+hipError_t launch_sum(const AttnShape& s, int G, int rows, int splits, const float* part, const View& out,
+                      hipStream_t st) {
+  const long total = (long)s.B * s.Hkv * rows, threads = total * (s.d / 4);
+  const auto k = s.bf16 ? attn_sum_kernel<bf16, 128>
+                        : s.d == 64 ? attn_sum_kernel<float, 64> : attn_sum_kernel<float, 128>;
+  hipLaunchKernelGGL(k, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, s.Hkv, G, rows, splits, total,
+                     part, out);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t attn_backward_workspace_bytes(const AttnShape& s) {
+  const GradPlan p = grad_plan(s);
+  return p.lsed + std::max(p.qpart, 2 * p.kpart);
+}
+
+hipError_t launch_attn_backward(const AttnShape& s, const HeadView& Q, const HeadView& K, const HeadView& V,
+                                const int32_t* kv_len, float scale, const HeadView& O, const float* lse,
+                                const HeadView& dO, const HeadView& dQ, const HeadView& dK,
+                                const HeadView& dV, void* ws, hipStream_t st) {
+  const GradPlan p = grad_plan(s);
+  GradArgs a{};
+  a.c = attn_call(s, Q, K, V, dO, kv_len, scale);
+  a.R = p.R, a.Np = p.Np;
+  float2* lseD = (float2*)ws;
+  a.lseD = lseD;
+  a.part = (float*)((char*)ws + p.lsed);
+  const long rows = (long)s.B * s.H * p.Np;
+  const dim3 rgrid((unsigned)((rows * 16 + 255) / 256));
+  if (s.bf16)
+    hipLaunchKernelGGL(attn_rowdot_bf16_kernel, rgrid, dim3(256), 0, st, s.H, s.Nq, p.Np, rows,
+                       view_of(O, true), a.c.O, lse, lseD);
+  else
+    hipLaunchKernelGGL(attn_rowdot_f32_kernel, rgrid, dim3(256), 0, st, s.H, s.Nq, p.Np, s.d, rows,
+                       view_of(O, false), a.c.O, lse, lseD);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const long bh = (long)s.B * s.Hkv;
+  a.G1 = view_of(dQ, s.bf16);
+  a.tiles = p.qtiles, a.splits = p.qsplits, a.total = (int)(bh * p.qtiles * p.qsplits);
+  const auto kq = s.bf16 ? attn_dq_bf16_kernel : s.d == 64 ? attn_dq_f32_kernel<64> : attn_dq_f32_kernel<128>;
+  hipLaunchKernelGGL(kq, dim3(a.total), dim3(256), 0, st, a);
+  e = hipGetLastError();
+  if (e == hipSuccess && p.qsplits > 1)
+    e = launch_sum(s, s.H / s.Hkv, p.R, p.qsplits, a.part, a.G1, st);
+  if (e != hipSuccess) return e;
+  a.G1 = view_of(dK, s.bf16), a.G2 = view_of(dV, s.bf16);
+  a.tiles = p.ktiles, a.splits = p.ksplits, a.total = (int)(bh * p.ktiles * p.ksplits);
+  a.part2 = (long)(p.kpart / sizeof(float));
+  if (s.bf16)
+    hipLaunchKernelGGL(attn_dkv_bf16_kernel, dim3(a.total), dim3(512), 0, st, a);
+  else
+    hipLaunchKernelGGL(s.d == 64 ? attn_dkv_f32_kernel<64> : attn_dkv_f32_kernel<128>, dim3(a.total), dim3(256),
+                       0, st, a);
+  e = hipGetLastError();
+  if (e == hipSuccess && p.ksplits > 1) {
+    e = launch_sum(s, 1, s.Nk, p.ksplits, a.part, a.G1, st);
+    if (e == hipSuccess) e = launch_sum(s, 1, s.Nk, p.ksplits, a.part + a.part2, a.G2, st);
+  }
+  return e;
+}
+
+}  // namespace rola

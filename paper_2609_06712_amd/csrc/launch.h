@@ -188,4 +188,40 @@ hipError_t launch_gate_backward(const Shape& s, const void* X, int d_model, cons
                                 const float* dlogits, float* dX, float* dWg, float* dbg, void* ws,
                                 hipStream_t st);
 
+// norm.hip: layer / RMS norm of `rows` rows of d channels (d % 8 == 0, <= norm_max_channels()), W and Bias
+// [groups, d], each for rows / groups consecutive rows; either may be null. Row strides in elements.
+struct NormShape {
+  long rows;
+  int d, groups;
+  bool bf16, wbf16, rms;  // element type; type of W and Bias; no mean
+};
+int norm_max_channels();
+// mean, rstd (fp32 [rows], either may be null): what the backward takes.
+hipError_t launch_norm(const NormShape& s, const void* X, long ldx, const void* W, const void* Bias,
+                       float eps, void* Y, long ldy, float* mean, float* rstd, hipStream_t st);
+size_t norm_backward_workspace_bytes(const NormShape& s);
+// dX in X's type; dW, dB fp32 [groups, d]; dB may be null, dW only with it.
+hipError_t launch_norm_backward(const NormShape& s, const void* X, long ldx, const void* W,
+                                const float* mean, const float* rstd, const void* dY, long ldy, void* dX,
+                                long lddx, float* dW, float* dB, void* ws, hipStream_t st);
+
+// attn.hip, attn_grad.hip: softmax attention of Nq queries over Nk keys in place, by strides.
+struct HeadView {
+  const void* p;
+  long b, h, n;  // element strides of a [B, H, N, d] tensor; the channels are consecutive
+};
+struct AttnShape {
+  int B, H, Hkv, Nq, Nk, d;
+  bool bf16, causal;
+};
+size_t attn_workspace_bytes(const AttnShape& s);
+hipError_t launch_attn(const AttnShape& s, const HeadView& Q, const HeadView& K, const HeadView& V,
+                       const int32_t* kv_len, float scale, const HeadView& O, float* lse, void* ws,
+                       hipStream_t st);
+size_t attn_backward_workspace_bytes(const AttnShape& s);
+hipError_t launch_attn_backward(const AttnShape& s, const HeadView& Q, const HeadView& K, const HeadView& V,
+                                const int32_t* kv_len, float scale, const HeadView& O, const float* lse,
+                                const HeadView& dO, const HeadView& dQ, const HeadView& dK,
+                                const HeadView& dV, void* ws, hipStream_t st);
+
 }  // namespace rola

@@ -213,6 +213,180 @@ rola_status run_combine(const rola::Shape& s, const void* Qr, const void* Kr, co
   return hip_status(e, fn);
 }
 
+// ---- tensors by strides (norms, attention over another set of tokens) ----------------------------
+
+// A [B, H, N] set of rows in place, in bytes.
+struct Rows {
+  const char* p;
+  long long size[3], stride[3], row;
+  const char* name;
+  long long end() const {  // bytes from the first element to behind the last
+    long long e = row;
+    for (int i = 0; i < 3; ++i) e += (size[i] - 1) * stride[i];
+    return e;
+  }
+};
+
+// Whether no element of an output is at two places.
+bool self_disjoint(const Rows& v) {
+  long long ext = v.row;
+  bool used[3] = {v.size[0] == 1, v.size[1] == 1, v.size[2] == 1};
+  for (int k = 0; k < 3; ++k) {
+    int best = -1;
+    for (int i = 0; i < 3; ++i)
+      if (!used[i] && (best < 0 || v.stride[i] < v.stride[best])) best = i;
+    if (best < 0) break;
+    used[best] = true;
+    if (v.stride[best] < ext) return false;
+    ext += (v.size[best] - 1) * v.stride[best];
+  }
+  return true;
+}
+
+// Whether two tensors may share bytes: their ranges meet, and they are not parts of one packed tensor whose
+// pieces (of a token, or of a sample) lie side by side within the same stride.
+bool rows_overlap(const Rows& a, const Rows& b) {
+  if (!overlap(a.p, (size_t)a.end(), b.p, (size_t)b.end())) return false;
+  for (int level : {2, 0}) {  // the token stride, the sample stride
+    const long long s = a.stride[level];
+    if (s <= 0 || s != b.stride[level]) continue;
+    // everything but the dimensions that step by multiples of s lies within one window of s
+    long long wa = a.row, wb = b.row;
+    bool ok = true;
+    for (int i = 0; i < 3; ++i) {
+      if (i == level) continue;
+      const bool whole_a = a.size[i] == 1 || a.stride[i] % s == 0;
+      const bool whole_b = b.size[i] == 1 || b.stride[i] % s == 0;
+      if (whole_a && whole_b && level == 2 && i == 0) continue;  // whole samples of tokens
+      wa += (a.size[i] - 1) * a.stride[i];
+      wb += (b.size[i] - 1) * b.stride[i];
+    }
+    ok = wa <= s && wb <= s;
+    if (!ok) continue;
+    const long long off = (((a.p - b.p) % s) + s) % s;  // a's window in b's frame
+    if (off >= wb && off + wa <= s) return false;
+  }
+  return true;
+}
+
+rola_status check_rows(const Rows& v, const char* fn) {
+  if (!aligned(v.p))
+    return fail(ROLA_ERR_INVALID_ARGUMENT, "%s: pointer '%s' is null or not 16-byte aligned", fn, v.name);
+  for (int i = 0; i < 3; ++i)
+    if (v.size[i] > 1 && (v.stride[i] < 0 || v.stride[i] % 16 != 0 || v.stride[i] >= 1ll << 40))
+      return fail(ROLA_ERR_INVALID_ARGUMENT, "%s: strides of %s must be multiples of 16 bytes, not negative",
+                  fn, v.name);
+  if (v.size[2] > 1 && v.stride[2] >= 1ll << 26)
+    return fail(ROLA_ERR_UNSUPPORTED, "%s: the token stride of %s must be below 2^26 bytes", fn, v.name);
+  return ROLA_OK;
+}
+
+rola_status check_disjoint(std::initializer_list<Rows> outs, std::initializer_list<Rows> ins, const char* fn) {
+  for (const Rows* o = outs.begin(); o != outs.end(); ++o) {
+    if (!o->p) continue;
+    if (!self_disjoint(*o))
+      return fail(ROLA_ERR_INVALID_ARGUMENT, "%s: output %s overlaps itself", fn, o->name);
+    for (const Rows* q = outs.begin(); q != o; ++q)
+      if (q->p && rows_overlap(*o, *q))
+        return fail(ROLA_ERR_INVALID_ARGUMENT, "%s: outputs %s and %s overlap", fn, q->name, o->name);
+    for (const Rows& in : ins)
+      if (in.p && rows_overlap(*o, in))
+        return fail(ROLA_ERR_INVALID_ARGUMENT, "%s: output %s overlaps %s", fn, o->name, in.name);
+  }
+  return ROLA_OK;
+}
+
+// A contiguous buffer (or none) as one row.
+Rows flat(const void* p, size_t bytes, const char* name) {
+  return Rows{(const char*)p, {1, 1, 1}, {0, 0, 0}, (long long)bytes, name};
+}
+size_t dtype_size(int32_t dtype) { return dtype == ROLA_DTYPE_BF16 ? 2 : 4; }
+
+rola_status check_norm(const rola_norm_problem* p, const char* fn, rola::NormShape* s) {
+  if (!p) return fail(ROLA_ERR_INVALID_ARGUMENT, "%s: problem is null", fn);
+  if (p->rows < 1 || p->groups < 1 || p->rows % p->groups != 0)
+    return fail(ROLA_ERR_INVALID_ARGUMENT, "%s: rows=%d must be a positive multiple of groups=%d", fn, p->rows,
+                p->groups);
+  if (p->d < 1 || p->d % 8 != 0)
+    return fail(ROLA_ERR_INVALID_ARGUMENT, "%s: d=%d must be a positive multiple of 8", fn, p->d);
+  if (p->kind != ROLA_NORM_LAYER && p->kind != ROLA_NORM_RMS)
+    return fail(ROLA_ERR_INVALID_ARGUMENT, "%s: unknown kind %d", fn, p->kind);
+  for (int32_t t : {p->dtype, p->wdtype})
+    if (t != ROLA_DTYPE_F32 && t != ROLA_DTYPE_BF16)
+      return fail(ROLA_ERR_INVALID_ARGUMENT, "%s: unknown dtype %d", fn, t);
+  if (p->dtype == ROLA_DTYPE_F32 && p->wdtype == ROLA_DTYPE_BF16)
+    return fail(ROLA_ERR_UNSUPPORTED, "%s: bf16 weights with fp32 rows", fn);
+  if (p->d > rola::norm_max_channels())
+    return fail(ROLA_ERR_UNSUPPORTED, "%s: d=%d above %d", fn, p->d, rola::norm_max_channels());
+  if (p->groups > 65535) return fail(ROLA_ERR_UNSUPPORTED, "%s: groups=%d above 65535", fn, p->groups);
+  *s = rola::NormShape{p->rows, p->d, p->groups, p->dtype == ROLA_DTYPE_BF16, p->wdtype == ROLA_DTYPE_BF16,
+                       p->kind == ROLA_NORM_RMS};
+  return ROLA_OK;
+}
+Rows norm_rows(const rola_norm_problem* p, const void* x, int64_t ld, const char* name) {
+  const long long e = (long long)dtype_size(p->dtype);
+  return Rows{(const char*)x, {1, 1, p->rows}, {0, 0, (long long)ld * e}, p->d * e, name};
+}
+// A stride in elements whose bytes would not fit is refused with the others.
+bool stride_fits(int64_t s) { return s >= 0 && s < (1ll << 40); }
+
+rola_status check_attn(const rola_attn_problem* p, const char* fn, rola::AttnShape* s) {
+  if (!p) return fail(ROLA_ERR_INVALID_ARGUMENT, "%s: problem is null", fn);
+  if (p->B < 1 || p->H < 1 || p->Hkv < 1 || p->Nq < 1 || p->Nk < 1)
+    return fail(ROLA_ERR_INVALID_ARGUMENT, "%s: sizes must be positive (B=%d H=%d Hkv=%d Nq=%d Nk=%d)", fn, p->B,
+                p->H, p->Hkv, p->Nq, p->Nk);
+  if (p->H % p->Hkv != 0)
+    return fail(ROLA_ERR_INVALID_ARGUMENT, "%s: H=%d must be a multiple of Hkv=%d", fn, p->H, p->Hkv);
+  if (p->dtype != ROLA_DTYPE_F32 && p->dtype != ROLA_DTYPE_BF16)
+    return fail(ROLA_ERR_INVALID_ARGUMENT, "%s: unknown dtype %d", fn, p->dtype);
+  if (p->causal != 0 && p->causal != 1)
+    return fail(ROLA_ERR_INVALID_ARGUMENT, "%s: causal must be 0 or 1", fn);
+  if (p->d_h != 128 && !(p->d_h == 64 && p->dtype == ROLA_DTYPE_F32))
+    return fail(ROLA_ERR_UNSUPPORTED, "%s: d_h=%d (built: 128, and 64 in fp32)", fn, p->d_h);
+  typedef unsigned __int128 u128;
+  const u128 most = 0x7fffffff;
+  // (the padded queries and keys, which the kernels index)
+  if ((u128)p->B * p->H * ((u128)p->Nq + 127) > most || (u128)p->B * p->Hkv * ((u128)p->Nk + 127) > most)
+    return fail(ROLA_ERR_UNSUPPORTED, "%s: B*H*Nq and B*Hkv*Nk must be below 2^31", fn);
+  *s = rola::AttnShape{p->B, p->H, p->Hkv, p->Nq, p->Nk, p->d_h, p->dtype == ROLA_DTYPE_BF16, p->causal == 1};
+  return ROLA_OK;
+}
+
+// One tensor of an attention call, checked: `rows` for the overlap checks, `view` for the launch.
+rola_status check_heads(const rola_heads* t, const rola_attn_problem* p, bool keys, const char* name,
+                        const char* fn, Rows* rows, rola::HeadView* view) {
+  if (!t) return fail(ROLA_ERR_INVALID_ARGUMENT, "%s: '%s' is null", fn, name);
+  const long long e = (long long)dtype_size(p->dtype);
+  for (int64_t s : {t->b, t->h, t->n})
+    if (!stride_fits(s)) return fail(ROLA_ERR_INVALID_ARGUMENT, "%s: strides of %s", fn, name);
+  *rows = Rows{(const char*)t->data,
+               {p->B, keys ? p->Hkv : p->H, keys ? p->Nk : p->Nq},
+               {t->b * e, t->h * e, t->n * e},
+               p->d_h * e,
+               name};
+  *view = rola::HeadView{t->data, t->b, t->h, t->n};
+  // a dimension of one has no stride
+  if (rows->size[0] == 1) rows->stride[0] = 0, view->b = 0;
+  if (rows->size[1] == 1) rows->stride[1] = 0, view->h = 0;
+  if (rows->size[2] == 1) rows->stride[2] = 0, view->n = 0;
+  return check_rows(*rows, fn);
+}
+
+rola_status check_attn_rest(const int32_t* kv_len, float scale, const char* fn) {
+  if (((uintptr_t)kv_len & 3u) != 0)
+    return fail(ROLA_ERR_INVALID_ARGUMENT, "%s: kv_len not 4-byte aligned", fn);
+  if (!(scale > 0.f) || !isfinite(scale))
+    return fail(ROLA_ERR_INVALID_ARGUMENT, "%s: softmax_scale must be finite and positive", fn);
+  return ROLA_OK;
+}
+
+rola_status check_ws(void* ws, size_t have, size_t need, const char* fn) {
+  if (need == 0) return ROLA_OK;
+  if (have < need) return fail(ROLA_ERR_WORKSPACE, "%s: workspace %zu bytes, need %zu", fn, have, need);
+  if (!aligned(ws)) return fail(ROLA_ERR_INVALID_ARGUMENT, "%s: pointer 'ws' is null or not 16-byte aligned", fn);
+  return ROLA_OK;
+}
+
 
 }  // namespace
 
@@ -846,6 +1020,130 @@ rola_status rola_lowrank_readout_combine(const rola_problem* p, const void* Qn, 
   return rola_lowrank_readout_combine_ex(p, Qn, Pq, r, cos_tab, sin_tab, rope_ld, ROLA_PHI_SILU,
                                          ROLA_ROPE_OUTSIDE, C, eps_lr, Os, gate_logits, eps, O,
                                          stream);
+}
+
+rola_status rola_norm(const rola_norm_problem* p, const void* X, int64_t ldx, const void* W,
+                      const void* Bias, float eps, void* Y, int64_t ldy, float* mean, float* rstd,
+                      hipStream_t stream) {
+  rola::NormShape s;
+  TRY(check_norm(p, __func__, &s));
+  if (!stride_fits(ldx) || !stride_fits(ldy))
+    return fail(ROLA_ERR_INVALID_ARGUMENT, "%s: row strides out of range", __func__);
+  const Rows x = norm_rows(p, X, ldx, "X"), y = norm_rows(p, Y, ldy, "Y");
+  TRY(check_rows(x, __func__));
+  TRY(check_rows(y, __func__));
+  const size_t wbytes = (size_t)p->groups * p->d * dtype_size(p->wdtype), sbytes = (size_t)p->rows * 4;
+  const void* ptrs[] = {W, Bias, mean, rstd};
+  const char* names[] = {"W", "Bias", "mean", "rstd"};
+  for (int i = 0; i < 4; ++i)
+    if (ptrs[i] && !aligned(ptrs[i]))
+      return fail(ROLA_ERR_INVALID_ARGUMENT, "%s: pointer '%s' is not 16-byte aligned", __func__, names[i]);
+  if (!(eps >= 0.f) || !isfinite(eps))
+    return fail(ROLA_ERR_INVALID_ARGUMENT, "%s: eps must be finite and >= 0", __func__);
+  TRY(check_disjoint({y, flat(mean, sbytes, "mean"), flat(rstd, sbytes, "rstd")},
+                     {x, flat(W, wbytes, "W"), flat(Bias, wbytes, "Bias")}, __func__));
+  return hip_status(rola::launch_norm(s, X, ldx, W, Bias, eps, Y, ldy, s.rms ? nullptr : mean, rstd, stream),
+                    __func__);
+}
+
+size_t rola_norm_backward_workspace_bytes(const rola_norm_problem* p) {
+  rola::NormShape s;
+  if (check_norm(p, __func__, &s) != ROLA_OK) return 0;
+  return rola::norm_backward_workspace_bytes(s);
+}
+
+rola_status rola_norm_backward(const rola_norm_problem* p, const void* X, int64_t ldx, const void* W,
+                               const float* mean, const float* rstd, const void* dY, int64_t ldy,
+                               void* dX, int64_t lddx, float* dW, float* dB, void* ws, size_t ws_bytes,
+                               hipStream_t stream) {
+  rola::NormShape s;
+  TRY(check_norm(p, __func__, &s));
+  if (!stride_fits(ldx) || !stride_fits(ldy) || !stride_fits(lddx))
+    return fail(ROLA_ERR_INVALID_ARGUMENT, "%s: row strides out of range", __func__);
+  const Rows x = norm_rows(p, X, ldx, "X"), dy = norm_rows(p, dY, ldy, "dY"), dx = norm_rows(p, dX, lddx, "dX");
+  TRY(check_rows(x, __func__));
+  TRY(check_rows(dy, __func__));
+  TRY(check_rows(dx, __func__));
+  REQUIRE_PTR(rstd);
+  if (!s.rms) REQUIRE_PTR(mean);
+  const void* ptrs[] = {W, dW, dB};
+  const char* names[] = {"W", "dW", "dB"};
+  for (int i = 0; i < 3; ++i)
+    if (ptrs[i] && !aligned(ptrs[i]))
+      return fail(ROLA_ERR_INVALID_ARGUMENT, "%s: pointer '%s' is not 16-byte aligned", __func__, names[i]);
+  if (dB && !dW) return fail(ROLA_ERR_INVALID_ARGUMENT, "%s: dB without dW", __func__);
+  const size_t need = rola::norm_backward_workspace_bytes(s);
+  TRY(check_ws(ws, ws_bytes, need, __func__));
+  const size_t wbytes = (size_t)p->groups * p->d * dtype_size(p->wdtype), sbytes = (size_t)p->rows * 4;
+  const size_t gbytes = (size_t)p->groups * p->d * 4;
+  TRY(check_disjoint({dx, flat(dW, gbytes, "dW"), flat(dB, gbytes, "dB"), flat(ws, need, "ws")},
+                     {x, dy, flat(W, wbytes, "W"), flat(s.rms ? nullptr : mean, sbytes, "mean"),
+                      flat(rstd, sbytes, "rstd")},
+                     __func__));
+  return hip_status(rola::launch_norm_backward(s, X, ldx, W, mean, rstd, dY, ldy, dX, lddx, dW, dB, ws, stream),
+                    __func__);
+}
+
+size_t rola_attn_workspace_bytes(const rola_attn_problem* p) {
+  rola::AttnShape s;
+  if (check_attn(p, __func__, &s) != ROLA_OK) return 0;
+  return rola::attn_workspace_bytes(s);
+}
+
+rola_status rola_attn(const rola_attn_problem* p, const rola_heads* Q, const rola_heads* K,
+                      const rola_heads* V, const int32_t* kv_len, float softmax_scale,
+                      const rola_heads* O, float* lse, void* ws, size_t ws_bytes, hipStream_t stream) {
+  rola::AttnShape s;
+  TRY(check_attn(p, __func__, &s));
+  Rows q, k, v, o;
+  rola::HeadView vq, vk, vv, vo;
+  TRY(check_heads(Q, p, false, "Q", __func__, &q, &vq));
+  TRY(check_heads(K, p, true, "K", __func__, &k, &vk));
+  TRY(check_heads(V, p, true, "V", __func__, &v, &vv));
+  TRY(check_heads(O, p, false, "O", __func__, &o, &vo));
+  TRY(check_attn_rest(kv_len, softmax_scale, __func__));
+  if (lse) REQUIRE_PTR(lse);
+  const size_t need = rola::attn_workspace_bytes(s);
+  TRY(check_ws(ws, ws_bytes, need, __func__));
+  TRY(check_disjoint({o, flat(lse, (size_t)p->B * p->H * p->Nq * 4, "lse"), flat(need ? ws : nullptr, need, "ws")},
+                     {q, k, v, flat(kv_len, (size_t)p->B * 4, "kv_len")}, __func__));
+  return hip_status(rola::launch_attn(s, vq, vk, vv, kv_len, softmax_scale, vo, lse, ws, stream), __func__);
+}
+
+size_t rola_attn_backward_workspace_bytes(const rola_attn_problem* p) {
+  rola::AttnShape s;
+  if (check_attn(p, __func__, &s) != ROLA_OK) return 0;
+  return rola::attn_backward_workspace_bytes(s);
+}
+
+rola_status rola_attn_backward(const rola_attn_problem* p, const rola_heads* Q, const rola_heads* K,
+                               const rola_heads* V, const int32_t* kv_len, float softmax_scale,
+                               const rola_heads* O, const float* lse, const rola_heads* dO,
+                               const rola_heads* dQ, const rola_heads* dK, const rola_heads* dV,
+                               void* ws, size_t ws_bytes, hipStream_t stream) {
+  rola::AttnShape s;
+  TRY(check_attn(p, __func__, &s));
+  Rows q, k, v, o, go, gq, gk, gv;
+  rola::HeadView vq, vk, vv, vo, wo, wq, wk, wv;
+  TRY(check_heads(Q, p, false, "Q", __func__, &q, &vq));
+  TRY(check_heads(K, p, true, "K", __func__, &k, &vk));
+  TRY(check_heads(V, p, true, "V", __func__, &v, &vv));
+  TRY(check_heads(O, p, false, "O", __func__, &o, &vo));
+  TRY(check_heads(dO, p, false, "dO", __func__, &go, &wo));
+  TRY(check_heads(dQ, p, false, "dQ", __func__, &gq, &wq));
+  TRY(check_heads(dK, p, true, "dK", __func__, &gk, &wk));
+  TRY(check_heads(dV, p, true, "dV", __func__, &gv, &wv));
+  TRY(check_attn_rest(kv_len, softmax_scale, __func__));
+  REQUIRE_PTR(lse);
+  const size_t need = rola::attn_backward_workspace_bytes(s);
+  TRY(check_ws(ws, ws_bytes, need, __func__));
+  TRY(check_disjoint({gq, gk, gv, flat(ws, need, "ws")},
+                     {q, k, v, o, go, flat(lse, (size_t)p->B * p->H * p->Nq * 4, "lse"),
+                      flat(kv_len, (size_t)p->B * 4, "kv_len")},
+                     __func__));
+  return hip_status(rola::launch_attn_backward(s, vq, vk, vv, kv_len, softmax_scale, vo, lse, wo, wq, wk, wv, ws,
+                                               stream),
+                    __func__);
 }
 
 }  // extern "C"

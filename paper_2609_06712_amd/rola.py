@@ -21,6 +21,7 @@ DTYPE_F32, DTYPE_BF16 = 0, 1
 
 # Every function include/rola.h declares, with (restype, argtypes).
 _p, _i32, _f32, _f64, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float, ctypes.c_double, ctypes.c_size_t
+_i64 = ctypes.c_int64
 
 
 class Problem(ctypes.Structure):
@@ -29,7 +30,25 @@ class Problem(ctypes.Structure):
                 ("T", _i32), ("Hs", _i32), ("Ws", _i32), ("dtype", _i32)]
 
 
+class NormProblem(ctypes.Structure):
+    """rola_norm_problem: rows of d channels, a weight per group of consecutive rows."""
+    _fields_ = [("rows", _i32), ("d", _i32), ("groups", _i32), ("kind", _i32), ("dtype", _i32),
+                ("wdtype", _i32)]
+
+
+class AttnProblem(ctypes.Structure):
+    """rola_attn_problem: Nq queries of H heads over Nk keys of Hkv heads."""
+    _fields_ = [("B", _i32), ("H", _i32), ("Hkv", _i32), ("Nq", _i32), ("Nk", _i32), ("d_h", _i32),
+                ("dtype", _i32), ("causal", _i32)]
+
+
+class Heads(ctypes.Structure):
+    """rola_heads: a [B, heads, N, d_h] tensor in place, strides in elements."""
+    _fields_ = [("data", _p), ("b", _i64), ("h", _i64), ("n", _i64)]
+
+
 _PP = ctypes.POINTER(Problem)
+_NP, _AP, _HP = ctypes.POINTER(NormProblem), ctypes.POINTER(AttnProblem), ctypes.POINTER(Heads)
 SIGNATURES = {
     "rola_num_blocks": (_i32, [_i32, _i32]),
     "rola_keep_blocks": (_i32, [_i32, _f64]),
@@ -79,6 +98,14 @@ SIGNATURES = {
                                                 _p, _p, _i32, _p, _f32, _p, _f32, _p, _p, _p]),
     "rola_sparse_attn_combine_planned": (_i32, [_PP, _p, _p, _p, _i32, _f64, _p, _f32, _p, _p, _i32,
                                                 _p, _p, _i32, _p, _f32, _p, _f32, _p, _p, _p, _sz, _p]),
+    "rola_norm": (_i32, [_NP, _p, _i64, _p, _p, _f32, _p, _i64, _p, _p, _p]),
+    "rola_norm_backward_workspace_bytes": (_sz, [_NP]),
+    "rola_norm_backward": (_i32, [_NP, _p, _i64, _p, _p, _p, _p, _i64, _p, _i64, _p, _p, _p, _sz, _p]),
+    "rola_attn_workspace_bytes": (_sz, [_AP]),
+    "rola_attn": (_i32, [_AP, _HP, _HP, _HP, _p, _f32, _HP, _p, _p, _sz, _p]),
+    "rola_attn_backward_workspace_bytes": (_sz, [_AP]),
+    "rola_attn_backward": (_i32, [_AP, _HP, _HP, _HP, _p, _f32, _HP, _p, _HP, _HP, _HP, _HP, _p, _sz,
+                                  _p]),
 }
 
 # Feature map and rotation order of the low-rank branch (rola_phi, rola_rope_order).
@@ -859,3 +886,262 @@ def rola_gate_logits_backward(X, Wg, dlogits, grid, H=1, d_h=128, want_dX=True, 
                                          _ptr(dX), _ptr(dWg), _ptr(dbg), _ptr(ws), ws.numel(),
                                          _stream(stream)), "rola_gate_logits_backward")
     return dX, dWg, dbg[:1]
+
+
+# ---- norms, and attention over another set of tokens (tensors in place, by strides) ----------------
+
+NORM_KIND = {"layer": 0, "rms": 1}
+
+
+def _on_current_device(x):
+    """The kernels run on the current device's stream."""
+    if x.get_device() != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {x.device}, the current device is "
+                         f"cuda:{torch.cuda.current_device()}")
+
+
+def _norm_rows(a, x, name, like=None):
+    """Row stride of a [rows, d] or [B, N, d] tensor whose rows follow each other at one stride."""
+    if not isinstance(x, torch.Tensor):
+        raise ValueError(f"{name} must be a tensor")
+    if like is None:
+        if x.dtype not in _ACT_DTYPES:
+            raise ValueError(f"{name} must be bfloat16 or float32, got {x.dtype}")
+        if x.dim() not in (2, 3):
+            raise ValueError(f"{name} must be [rows, d] or [B, N, d], got shape {tuple(x.shape)}")
+        if x.numel() == 0:
+            raise ValueError(f"{name} is empty: shape {tuple(x.shape)}")
+    else:
+        if x.dtype != like.dtype:
+            raise ValueError(f"{name} must be {like.dtype}, got {x.dtype}")
+        if x.shape != like.shape:
+            raise ValueError(f"{name} must have shape {tuple(like.shape)}, got {tuple(x.shape)}")
+    ld, d = x.stride(-2), x.shape[-1]
+    if x.dim() == 3:
+        if x.shape[1] == 1:
+            ld = x.stride(0)
+        elif x.shape[0] > 1 and x.stride(0) != x.shape[1] * ld:
+            raise ValueError(f"{name}: the rows must follow each other at one stride, got strides {x.stride()}")
+    if x.numel() == d:  # one row
+        ld = d
+    a.placed.append((x, name, d > 1))
+    return ld
+
+
+def _norm_params(a, x, w, name, dtype=None):
+    """Groups of rows that a weight [d], or [B, d] for x [B, N, d], gives."""
+    if w is None:
+        return None
+    if not isinstance(w, torch.Tensor):
+        raise ValueError(f"{name} must be a tensor")
+    if dtype is None and w.dtype != torch.float32 and w.dtype != x.dtype:
+        raise ValueError(f"{name} must be float32 or {x.dtype}, got {w.dtype}")
+    d = x.shape[-1]
+    per_sample = w.dim() == 2 and x.dim() == 3
+    a.tensor(w, name, (x.shape[0], d) if per_sample else (d,), dtype or w.dtype)
+    return x.shape[0] if per_sample else 1
+
+
+@functools.lru_cache(maxsize=1024)
+def _norm_problem(rows, d, groups, kind, dtype, wdtype) -> NormProblem:
+    return NormProblem(rows, d, groups, kind, dtype, wdtype)
+
+
+@functools.lru_cache(maxsize=1024)
+def _norm_ws(rows, d, groups, kind, dtype, wdtype):
+    return LIB.rola_norm_backward_workspace_bytes(
+        ctypes.byref(_norm_problem(rows, d, groups, kind, dtype, wdtype)))
+
+
+def _norm_key(x, w, groups, kind):
+    d = x.shape[-1]
+    wt = _DTYPE_CODES[x.dtype if w is None else w.dtype]
+    return x.numel() // d, d, groups or 1, NORM_KIND[kind], _DTYPE_CODES[x.dtype], wt
+
+
+def rola_norm(X, W=None, Bias=None, kind="layer", eps=1e-6, out=None, want_stats=False, stream=None):
+    """Layer norm ("layer") or RMS norm ("rms") of X [rows, d] or [B, N, d] (rows at one stride) with
+    W and Bias [d], or [B, d] for a weight per sample; either may be None. Returns Y, or with want_stats
+    (Y, mean, rstd), the fp32 statistics per row that rola_norm_backward takes (mean None for "rms")."""
+    if kind not in NORM_KIND:
+        raise ValueError(f"kind must be one of {sorted(NORM_KIND)}, got {kind!r}")
+    a = _Args()
+    ldx = _norm_rows(a, X, "X")
+    groups = _norm_params(a, X, W, "W")
+    if Bias is not None:
+        gb = _norm_params(a, X, Bias, "Bias", None if W is None else W.dtype)
+        if groups is not None and gb != groups:
+            raise ValueError("W and Bias must have the same shape")
+        groups = gb
+    if out is None:
+        out, ldy = torch.empty(X.shape, dtype=X.dtype, device=X.device), X.shape[-1]
+    else:
+        ldy = _norm_rows(a, out, "out", X)
+    a.done()
+    _on_current_device(X)
+    mean = rstd = None
+    if want_stats:
+        rstd = torch.empty(X.shape[:-1], dtype=torch.float32, device=X.device)
+        mean = torch.empty_like(rstd) if kind == "layer" else None
+    prob = _norm_problem(*_norm_key(X, Bias if W is None else W, groups, kind))
+    _check(LIB.rola_norm(prob, _ptr(X), ldx, _ptr(W), _ptr(Bias), eps, _ptr(out), ldy, _ptr(mean), _ptr(rstd),
+                         _stream(stream)), "rola_norm")
+    return (out, mean, rstd) if want_stats else out
+
+
+def norm_backward_workspace_bytes(X, W=None, kind="layer") -> int:
+    return _norm_ws(*_norm_key(X, W, X.shape[0] if W is not None and W.dim() == 2 and X.dim() == 3 else 1,
+                               kind))
+
+
+def rola_norm_backward(X, W, mean, rstd, dY, kind="layer", want_bias=True, per_sample=None, out=None, ws=None,
+                       stream=None):
+    """(dX in X's type, dW, dB fp32 in W's shape; dB None without want_bias) of rola_norm, from the
+    statistics it kept. Without W (None) dW is that of a weight of ones; per_sample then says whether it (and
+    dB) is [B, d] instead of [d]."""
+    if kind not in NORM_KIND:
+        raise ValueError(f"kind must be one of {sorted(NORM_KIND)}, got {kind!r}")
+    a = _Args()
+    ldx = _norm_rows(a, X, "X")
+    ldy = _norm_rows(a, dY, "dY", X)
+    groups = _norm_params(a, X, W, "W")
+    if groups is None:
+        groups = X.shape[0] if per_sample and X.dim() == 3 else 1
+    elif per_sample is not None and bool(per_sample) != (W.dim() == 2):
+        raise ValueError("per_sample goes by W's shape when W is given")
+    for t, name in ((mean, "mean"), (rstd, "rstd")):
+        if name == "rstd" or kind == "layer":
+            a.tensor(t, name, X.shape[:-1], torch.float32)
+    if out is None:
+        out, ldo = torch.empty(X.shape, dtype=X.dtype, device=X.device), X.shape[-1]
+    else:
+        ldo = _norm_rows(a, out, "out", X)
+    key = _norm_key(X, W, groups, kind)
+    if ws is None:
+        ws = torch.empty(max(_norm_ws(*key), 16), dtype=torch.uint8, device=X.device)
+    a.workspace(ws)
+    a.done()
+    _on_current_device(X)
+    d = X.shape[-1]
+    shape = (2, d) if groups == 1 else (2, groups, d)
+    both = torch.empty(shape, dtype=torch.float32, device=X.device)
+    if W is not None and W.dim() == 2 or (W is None and per_sample and X.dim() == 3):
+        both = both.view(2, groups, d)
+    dW, dB = both[0], both[1] if want_bias else None
+    _check(LIB.rola_norm_backward(_norm_problem(*key), _ptr(X), ldx, _ptr(W),
+                                  _ptr(mean) if kind == "layer" else None, _ptr(rstd), _ptr(dY), ldy, _ptr(out),
+                                  ldo, _ptr(dW), _ptr(dB), _ptr(ws), ws.numel(), _stream(stream)),
+           "rola_norm_backward")
+    return out, dW, dB
+
+
+@functools.lru_cache(maxsize=1024)
+def _attn_problem(B, H, Hkv, Nq, Nk, d, dtype, causal) -> AttnProblem:
+    return AttnProblem(B, H, Hkv, Nq, Nk, d, dtype, causal)
+
+
+@functools.lru_cache(maxsize=1024)
+def _attn_ws(backward, *key):
+    fn = LIB.rola_attn_backward_workspace_bytes if backward else LIB.rola_attn_workspace_bytes
+    return fn(ctypes.byref(_attn_problem(*key)))
+
+
+def _in_place(a, x, name, shape, dtype):
+    """A [B, heads, N, d_h] tensor taken by its strides."""
+    if not isinstance(x, torch.Tensor):
+        raise ValueError(f"{name} must be a tensor")
+    if x.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {x.dtype}")
+    if x.shape != shape and tuple(x.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(x.shape)}")
+    a.placed.append((x, name, True))
+    s = x.stride()
+    return Heads(x.data_ptr(), s[0], s[1], s[2])
+
+
+def _like_heads(x, shape=None):
+    """An output in x's order of heads and tokens: token after token (the heads of a token beside each
+    other) where x has its heads inside its tokens, head after head otherwise."""
+    B, H, N, d = x.shape if shape is None else shape
+    if x.shape[1] > 1 and x.shape[2] > 1 and x.stride(1) < x.stride(2):
+        return torch.empty((B, N, H, d), dtype=x.dtype, device=x.device).transpose(1, 2)
+    return torch.empty((B, H, N, d), dtype=x.dtype, device=x.device)
+
+
+def _attn_args(a, Q, K, V, kv_len, causal):
+    for t, name in ((Q, "Q"), (K, "K")):
+        if not isinstance(t, torch.Tensor) or t.dim() != 4:
+            raise ValueError(f"{name} must be a [B, heads, N, d_h] tensor")
+    if Q.dtype not in _ACT_DTYPES:
+        raise ValueError(f"Q must be bfloat16 or float32, got {Q.dtype}")
+    B, H, Nq, d = Q.shape
+    Hkv, Nk = K.shape[1], K.shape[2]
+    if Q.numel() == 0 or K.numel() == 0:
+        raise ValueError(f"empty tensors: Q {tuple(Q.shape)}, K {tuple(K.shape)}")
+    hq = _in_place(a, Q, "Q", Q.shape, Q.dtype)
+    hk = _in_place(a, K, "K", (B, Hkv, Nk, d), Q.dtype)
+    hv = _in_place(a, V, "V", (B, Hkv, Nk, d), Q.dtype)
+    if kv_len is not None:
+        a.tensor(kv_len, "kv_len", (B,), torch.int32)
+    return (B, H, Hkv, Nq, Nk, d, _DTYPE_CODES[Q.dtype], 1 if causal else 0), hq, hk, hv
+
+
+def attn_workspace_bytes(Q, K, causal=False, backward=False) -> int:
+    """Workspace of rola_attn, or of rola_attn_backward, for tensors of these shapes."""
+    B, H, Nq, d = Q.shape
+    return _attn_ws(bool(backward), B, H, K.shape[1], Nq, K.shape[2], d, _DTYPE_CODES[Q.dtype],
+                    1 if causal else 0)
+
+
+def rola_attn(Q, K, V, kv_len=None, causal=False, scale=None, out=None, lse=None, want_lse=True, ws=None,
+              stream=None):
+    """(O, lse): softmax attention of Q [B, H, Nq, d_h] over K, V [B, Hkv, Nk, d_h], H a multiple of
+    Hkv. kv_len (int32 [B], on the device): keys per sample; causal: query i sees keys
+    j <= i + kv_len - Nq. Tensors are taken in place by their strides (unit inner stride), so views of packed
+    projections need no copy; O comes in Q's order of heads and tokens. lse: fp32 [B, H, Nq], log2 of
+    the softmax denominator of the log2e-scaled scores (None without want_lse)."""
+    a = _Args()
+    key, hq, hk, hv = _attn_args(a, Q, K, V, kv_len, causal)
+    if out is None:
+        out = _like_heads(Q)
+    ho = _in_place(a, out, "out", Q.shape, Q.dtype)
+    if lse is not None:
+        a.tensor(lse, "lse", Q.shape[:3], torch.float32)
+    elif want_lse:
+        lse = torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device)
+    need = _attn_ws(False, *key)
+    if ws is None and need:
+        ws = torch.empty(need, dtype=torch.uint8, device=Q.device)
+    a.workspace(ws)
+    a.done()
+    _on_current_device(Q)
+    _check(LIB.rola_attn(_attn_problem(*key), hq, hk, hv, _ptr(kv_len),
+                         key[5] ** -0.5 if scale is None else scale, ho, _ptr(lse), _ptr(ws),
+                         0 if ws is None else ws.numel(), _stream(stream)), "rola_attn")
+    return out, lse
+
+
+def rola_attn_backward(Q, K, V, O, lse, dO, kv_len=None, causal=False, scale=None, dQ=None, dK=None, dV=None,
+                       ws=None, stream=None):
+    """(dQ, dK, dV) of rola_attn in the inputs' type, from its O and lse; kv_len, causal and scale as in
+    the forward. Outputs come in the order of heads and tokens of Q, K and V, or are the tensors given."""
+    a = _Args()
+    key, hq, hk, hv = _attn_args(a, Q, K, V, kv_len, causal)
+    ho = _in_place(a, O, "O", Q.shape, Q.dtype)
+    hg = _in_place(a, dO, "dO", Q.shape, Q.dtype)
+    a.tensor(lse, "lse", Q.shape[:3], torch.float32)
+    dQ = _like_heads(Q) if dQ is None else dQ
+    dK = _like_heads(K) if dK is None else dK
+    dV = _like_heads(V) if dV is None else dV
+    gq = _in_place(a, dQ, "dQ", Q.shape, Q.dtype)
+    gk = _in_place(a, dK, "dK", K.shape, Q.dtype)
+    gv = _in_place(a, dV, "dV", K.shape, Q.dtype)
+    if ws is None:
+        ws = torch.empty(_attn_ws(True, *key), dtype=torch.uint8, device=Q.device)
+    a.workspace(ws)
+    a.done()
+    _on_current_device(Q)
+    _check(LIB.rola_attn_backward(_attn_problem(*key), hq, hk, hv, _ptr(kv_len),
+                                  key[5] ** -0.5 if scale is None else scale, ho, _ptr(lse), hg, gq, gk, gv,
+                                  _ptr(ws), ws.numel(), _stream(stream)), "rola_attn_backward")
+    return dQ, dK, dV

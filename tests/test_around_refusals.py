@@ -1,0 +1,162 @@
+"""Refusals of the norms and of the attention over another set of tokens: host checks, no launch."""
+
+import ctypes
+
+import pytest
+import torch
+
+R = pytest.importorskip("paper_2609_06712_amd.rola")
+
+no_gpu = pytest.mark.skipif(torch.cuda.device_count() > 0, reason="host-validation test: CPU only")
+INV, UNS, WS = R.ROLA_ERR_INVALID_ARGUMENT, R.ROLA_ERR_UNSUPPORTED, R.ROLA_ERR_WORKSPACE
+GB = 1 << 36
+
+
+def at(k, off=0):
+    """A distinct aligned address that is never read."""
+    return (k + 1) * GB + off
+
+
+def norm_call(rows=64, d=128, groups=1, kind=0, dt=1, wdt=0, X=at(0), ldx=128, W=at(1), Bias=at(2), eps=1e-6,
+              Y=at(3), ldy=128, mean=at(4), rstd=at(5)):
+    return R.LIB.rola_norm(R.NormProblem(rows, d, groups, kind, dt, wdt), X, ldx, W, Bias, eps, Y, ldy, mean,
+                           rstd, None)
+
+
+@no_gpu
+@pytest.mark.parametrize("status,kw", [
+    (INV, dict(rows=0)), (INV, dict(groups=0)), (INV, dict(groups=3)), (INV, dict(d=0)), (INV, dict(d=12)),
+    (INV, dict(kind=2)), (INV, dict(dt=2)), (INV, dict(wdt=5)), (UNS, dict(dt=0, wdt=1)),
+    (UNS, dict(d=16392, ldx=16392, ldy=16392)), (UNS, dict(rows=65536, groups=65536)),
+    (INV, dict(X=None)), (INV, dict(Y=None)), (INV, dict(X=at(0, 8))), (INV, dict(W=at(1, 4))),
+    (INV, dict(rstd=at(5, 8))), (INV, dict(eps=-1.0)), (INV, dict(eps=float("nan"))), (INV, dict(ldx=132)),
+    (INV, dict(ldx=-128)), (INV, dict(ldy=120)), (INV, dict(Y=at(0))), (INV, dict(Y=at(0, 256))),
+    (INV, dict(mean=at(5))), (INV, dict(rstd=at(2))), (UNS, dict(ldx=1 << 26)), (INV, dict(ldy=1 << 60)),
+])
+def test_norm_refuses(status, kw):
+    assert norm_call(**kw) == status
+
+
+@no_gpu
+def test_norm_output_between_the_rows_of_its_packed_input():
+    """Parts of one packed row lie side by side; a part of the same columns does not."""
+    for off, want in ((128 * 2, None), (0, INV), (64 * 2, INV), (192 * 2, INV)):
+        # an accepted call would launch: only its check is asked for, with an unsupported width behind it
+        got = norm_call(X=at(0), ldx=256, Y=at(0, off), ldy=256, rows=32, mean=at(5) if want is None else at(4))
+        assert got == INV
+        message = R.LIB.rola_last_error().decode()
+        assert ("overlaps X" in message) == (want is not None), (off, message)
+
+
+def norm_grad_call(W=at(1), mean=at(2), rstd=at(3), dY=at(4), dX=at(5), dW=at(6), dB=at(7), ws=at(8),
+                   nbytes=1 << 30, kind=0, X=at(0), lddx=128):
+    return R.LIB.rola_norm_backward(R.NormProblem(64, 128, 1, kind, 1, 0), X, 128, W, mean, rstd, dY, 128, dX,
+                                    lddx, dW, dB, ws, nbytes, None)
+
+
+@no_gpu
+@pytest.mark.parametrize("status,kw", [
+    (INV, dict(mean=None)), (INV, dict(rstd=None)), (INV, dict(dY=None)), (INV, dict(dX=None)),
+    (INV, dict(dW=None)), (INV, dict(ws=None)), (INV, dict(ws=at(8, 8))), (WS, dict(nbytes=64)),
+    (INV, dict(dX=at(0))), (INV, dict(dX=at(4))), (INV, dict(dW=at(7))), (INV, dict(dB=at(6, 256))),
+    (INV, dict(ws=at(5))), (INV, dict(lddx=0)), (INV, dict(dB=at(7, 4))), (INV, dict(mean=None, kind=0)),
+])
+def test_norm_backward_refuses(status, kw):
+    assert norm_grad_call(**kw) == status
+
+
+def heads(k, b=0, h=1 << 16, n=128, off=0):
+    return R.Heads(at(k, off) if k is not None else None, b, h, n)
+
+
+def attn_call(B=1, H=2, Hkv=2, Nq=64, Nk=96, d=128, dt=1, causal=0, Q=heads(0), K=heads(1), V=heads(2), kv=at(3),
+              scale=0.1, O=heads(4), lse=at(5), ws=at(6), nbytes=1 << 32):
+    return R.LIB.rola_attn(R.AttnProblem(B, H, Hkv, Nq, Nk, d, dt, causal), Q, K, V, kv, scale, O, lse, ws, nbytes,
+                           None)
+
+
+@no_gpu
+@pytest.mark.parametrize("status,kw", [
+    (INV, dict(B=0)), (INV, dict(H=3)), (INV, dict(Hkv=0)), (INV, dict(Nq=0)), (INV, dict(Nk=0)),
+    (INV, dict(dt=2)), (INV, dict(causal=2)), (UNS, dict(d=64)), (UNS, dict(d=96)), (UNS, dict(d=96, dt=0)),
+    (UNS, dict(B=1 << 12, Nq=1 << 20)), (UNS, dict(B=1 << 12, Nk=1 << 20)),
+    (INV, dict(Q=heads(None))), (INV, dict(K=heads(1, off=8))), (INV, dict(V=heads(2, n=124))),
+    (INV, dict(V=heads(2, h=-128))), (UNS, dict(K=heads(1, n=1 << 25))), (INV, dict(O=heads(4, n=1 << 62))),
+    (INV, dict(kv=at(3, 2))), (INV, dict(scale=0.0)), (INV, dict(scale=float("inf"))),
+    (INV, dict(lse=at(5, 4))), (INV, dict(O=heads(0))), (INV, dict(O=heads(1, off=4096))),
+    (INV, dict(O=heads(4, n=0))), (INV, dict(O=heads(4, h=64))), (INV, dict(lse=at(4))), (INV, dict(lse=at(3))),
+    (WS, dict(Nk=4096, nbytes=16)), (INV, dict(Nk=4096, ws=None)), (INV, dict(Nk=4096, ws=at(0))),
+])
+def test_attn_refuses(status, kw):
+    assert attn_call(**kw) == status
+
+
+def grad_call(Q=heads(0), K=heads(1), V=heads(2), O=heads(3), lse=at(4), dO=heads(5), dQ=heads(6), dK=heads(7),
+              dV=heads(8), ws=at(9), nbytes=1 << 32, scale=0.1):
+    return R.LIB.rola_attn_backward(R.AttnProblem(1, 2, 2, 64, 96, 128, 1, 0), Q, K, V, None, scale, O, lse, dO,
+                                    dQ, dK, dV, ws, nbytes, None)
+
+
+@no_gpu
+@pytest.mark.parametrize("status,kw", [
+    (INV, dict(lse=None)), (INV, dict(dO=heads(None))), (INV, dict(dQ=heads(5))), (INV, dict(dK=heads(8))),
+    (INV, dict(dV=heads(2))), (INV, dict(dK=heads(7, n=0))), (INV, dict(ws=None)), (WS, dict(nbytes=0)),
+    (INV, dict(ws=at(6))), (INV, dict(scale=-1.0)), (INV, dict(dQ=heads(3, off=512))), (INV, dict(dV=heads(8, off=4))),
+])
+def test_attn_backward_refuses(status, kw):
+    assert grad_call(**kw) == status
+
+
+@no_gpu
+def test_packed_gradients_are_told_from_overlapping_ones():
+    """dQ, dK, dV as parts of one [N, 3, H, d] tensor pass the overlap check; shifted by half a head
+    they do not (the call that passes is stopped by its workspace)."""
+    part = lambda i, off=0: heads(6, h=128, n=3 * 256, off=i * 512 + off)
+    sq = R.AttnProblem(1, 2, 2, 64, 64, 128, 1, 0)
+    for shift, message in ((0, "output ws"), (128, "outputs dQ and dK")):
+        got = R.LIB.rola_attn_backward(sq, heads(0), heads(1), heads(2), None, 0.1, heads(3), at(4), heads(5),
+                                       part(0), part(1, -shift), part(2), at(0), 1 << 32, None)
+        assert got == INV and message in R.LIB.rola_last_error().decode(), R.LIB.rola_last_error()
+
+
+@no_gpu
+def test_workspace_sizes():
+    need = lambda fn, *p: fn(ctypes.byref(R.AttnProblem(*p)))
+    fwd, bwd = R.LIB.rola_attn_workspace_bytes, R.LIB.rola_attn_backward_workspace_bytes
+    assert need(fwd, 1, 12, 12, 32760, 512, 128, 1, 0) == 0       # the chip is full without a split
+    assert need(fwd, 1, 8, 1, 1, 32760, 128, 1, 0) > 0
+    assert need(bwd, 1, 12, 12, 32760, 512, 128, 1, 0) >= 12 * 32768 * 8
+    assert need(fwd, 1, 8, 3, 1, 32760, 128, 1, 0) == 0 and need(bwd, 1, 8, 3, 1, 32760, 128, 1, 0) == 0
+    assert R.LIB.rola_norm_backward_workspace_bytes(ctypes.byref(R.NormProblem(0, 8, 1, 0, 1, 0))) == 0
+    assert R.LIB.rola_norm_backward_workspace_bytes(ctypes.byref(R.NormProblem(64, 128, 1, 0, 1, 0))) >= 1024
+
+
+BF, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.mark.parametrize("change", [
+    dict(X=torch.zeros(2, 8, 4, 64)), dict(X=torch.zeros((2, 8, 64), dtype=torch.float16)),
+    dict(X=torch.zeros(0, 8, 64)), dict(X=torch.zeros(2, 16, 64)[:, ::2][:, :7]), dict(X=torch.zeros(2, 64, 8).transpose(1, 2)),
+    dict(W=torch.zeros(63)), dict(W=torch.zeros(3, 64)), dict(W=torch.zeros(64, dtype=BF)),
+    dict(Bias=torch.zeros(2, 64)), dict(kind="batch"), dict(out=torch.zeros(2, 8, 63)), dict(W=torch.zeros(64).double()),
+    dict(), # tensors that are not on a device
+])
+def test_binding_refuses_norm(change):
+    args = dict(X=torch.zeros(2, 8, 64), W=torch.ones(64), Bias=torch.zeros(64))
+    args.update(change)
+    with pytest.raises(ValueError):
+        R.rola_norm(**args)
+
+
+@pytest.mark.parametrize("change", [
+    dict(Q=torch.zeros(1, 2, 8)), dict(Q=torch.zeros(1, 2, 8, 128).half()), dict(Q=torch.zeros(1, 2, 0, 128)),
+    dict(K=torch.zeros(1, 2, 9, 64)), dict(K=torch.zeros(2, 2, 9, 128)), dict(V=torch.zeros(1, 2, 8, 128)),
+    dict(V=torch.zeros((1, 2, 9, 128), dtype=BF)), dict(Q=torch.zeros(1, 2, 128, 8).transpose(2, 3)),
+    dict(kv_len=torch.zeros(2, dtype=torch.int32)), dict(kv_len=torch.zeros(1, dtype=torch.int64)), dict(kv_len=9),
+    dict(out=torch.zeros(1, 2, 9, 128)), dict(lse=torch.zeros(1, 2, 9)), dict(ws=torch.zeros(8)), dict(),
+])
+def test_binding_refuses_attn(change):
+    args = dict(Q=torch.zeros(1, 2, 8, 128), K=torch.zeros(1, 2, 9, 128), V=torch.zeros(1, 2, 9, 128))
+    args.update(change)
+    with pytest.raises(ValueError):
+        R.rola_attn(**args)
