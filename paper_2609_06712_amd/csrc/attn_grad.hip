@@ -6,8 +6,13 @@
 // per block of keys (dK, dV, four). Bound by the matrix cores (14 d operations per visible pair against the ten
 // of a single pass, which would have to add dQ in memory).
 //
-// Row statistics: attn_rowdot_kernel packs {lse, D} per query, per head padded to whole tiles of 32 with
-// {inf, 0}: P is then zero for rows past the last and for rows that see no key, with no test in the walk.
+// D. It is rowsum(dO O), but from an O that was rounded to bf16 it is off by dO times that rounding, for all
+// keys of a row alike: sum_j P_ij K_j times the error reaches dQ, where sum_j dS_ij K_j has cancelled (8400 keys:
+// dQ off by 0.0048 of its norm, where its own rounding is 0.0017). So bf16 sums it in fp32 from what the
+// gradients use, D = rowsum(P dP), in a pass of two products (attn_rowsum_bf16_kernel); fp32 takes dO O.
+//
+// Row statistics: per query lse and D, in tiles of 32 queries [32 lse][32 D], per head padded to whole tiles with
+// lse = inf: P is then zero for rows past the last and for rows that see no key, with no test in the walk.
 //
 // When a pass has too few workgroups for the chip, each tile's walk is cut into parts whose fp32 sums go to the
 // workspace and are added in order by attn_sum_kernel.
@@ -25,40 +30,41 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 struct GradArgs {
   AttnCall c;     // c.O: dO
   View G1, G2;    // dQ; or dK, dV
-  int tiles, splits, total, R, Np;
-  const float2* lseD;  // [B, H, Np]
+  int tiles, splits, total, R, Np, H;
+  const float* stat;   // [B, H, Np / 32][lse, D][32]
+  const float* lse;    // [B, H, Nq], the forward's
   float* part;         // splits > 1: [B Hkv][splits][rows][d], dV's after dK's
   long part2;          // elements between dK's and dV's partials
 };
 
-__global__ __launch_bounds__(256) void attn_rowdot_bf16_kernel(int H, int Nq, int Np, long rows, View O, View dO,
-                                                               const float* __restrict__ lse,
-                                                               float2* __restrict__ lseD) {
-  const long row = ((long)blockIdx.x * 256 + threadIdx.x) / 16;  // (b, h, padded query)
-  const int part = threadIdx.x % 16;
+// Where the statistics of query i of a head are: lse there, D 32 further.
+__device__ __forceinline__ long stat_at(long head, int Np, int i) { return (head * (Np / 32) + i / 32) * 64 + i % 32; }
+
+// lse and D = the sum of `splits` parts [bh][split][R] (row i G + g of the key head bh) into tiles.
+__global__ __launch_bounds__(256) void attn_stat_kernel(int H, int G, int Nq, int Np, int splits, long rows,
+                                                        const float* __restrict__ lse,
+                                                        const float* __restrict__ part, float* __restrict__ stat) {
+  const long row = (long)blockIdx.x * 256 + threadIdx.x;  // (b, h, padded query)
   if (row >= rows) return;
   const long bh = row / Np;
-  const int i = (int)(row % Np), b = (int)(bh / H), h = (int)(bh % H);
-  float s = 0.f;
+  const int i = (int)(row % Np);
+  float l = -__builtin_inff(), s = 0.f;
   if (i < Nq) {
-    float x[8], y[8];
-    load8(reinterpret_cast<const bf16*>(O.p + b * O.b + h * O.h + i * O.n) + part * 8, x);
-    load8(reinterpret_cast<const bf16*>(dO.p + b * dO.b + h * dO.h + i * dO.n) + part * 8, y);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) s = fmaf(x[k], y[k], s);
+    l = lse[bh * Nq + i];
+    const int h = (int)(bh % H);
+    const long R = (long)Nq * G;
+    const float* p = part + (bh / H * (H / G) + h / G) * splits * R + (long)i * G + h % G;
+    for (int k = 0; k < splits; ++k) s += p[k * R];
   }
-#pragma unroll
-  for (int off = 8; off >= 1; off >>= 1) s += __shfl_xor(s, off, 16);
-  if (part == 0) {
-    const float l = i < Nq ? lse[bh * Nq + i] : -__builtin_inff();
-    const bool none = l == -__builtin_inff();
-    lseD[row] = make_float2(none ? __builtin_inff() : l, none ? 0.f : s);
-  }
+  const bool none = l == -__builtin_inff();
+  float* at = stat + stat_at(bh, Np, i);
+  at[0] = none ? __builtin_inff() : l;
+  at[32] = none ? 0.f : s;
 }
 
 __global__ __launch_bounds__(256) void attn_rowdot_f32_kernel(int H, int Nq, int Np, int d, long rows, View O,
                                                               View dO, const float* __restrict__ lse,
-                                                              float2* __restrict__ lseD) {
+                                                              float* __restrict__ stat) {
   const long row = ((long)blockIdx.x * 256 + threadIdx.x) / 16;
   const int part = threadIdx.x % 16;
   if (row >= rows) return;
@@ -78,7 +84,9 @@ __global__ __launch_bounds__(256) void attn_rowdot_f32_kernel(int H, int Nq, int
   if (part == 0) {
     const float l = i < Nq ? lse[bh * Nq + i] : -__builtin_inff();
     const bool none = l == -__builtin_inff();
-    lseD[row] = make_float2(none ? __builtin_inff() : l, none ? 0.f : s);
+    float* at = stat + stat_at(bh, Np, i);
+    at[0] = none ? __builtin_inff() : l;
+    at[32] = none ? 0.f : s;
   }
 }
 
@@ -112,8 +120,131 @@ __device__ __forceinline__ void store_row_bf16(char* row, const f32x16 (&acc)[4]
     }
 }
 
+// D = rowsum(P dP): four waves of 64 rows walk the keys in sub-tiles of 32 through three LDS stages. Two row
+// tiles per wave: an operand read from LDS serves two products, and without a gradient's accumulators two
+// workgroups fit a CU.
+__global__ __launch_bounds__(256, 2) void attn_rowsum_bf16_kernel(const GradArgs a) {
+  constexpr int STAGE = 2 * kTile, NBUF = 3, DPW = 2;
+  __shared__ __attribute__((aligned(1024))) char lds[NBUF * STAGE];
+  const AttnCall& c = a.c;
+  const Part pt = part_of(a, xcd_remap(blockIdx.x, a.total), c.causal);
+  const int wave = wave_uniform(threadIdx.x / 64), lane = threadIdx.x % 64, hh = lane / 32;
+  const int n = attn_keys(c, pt.b);
+  const int row0 = (pt.tile * 4 + wave) * 64;
+  const int lim_lo = attn_limit(c, n, min(row0, a.R - 1) / c.G);
+  const int lim_hi = row0 < a.R ? attn_limit(c, n, min(row0 + 63, a.R - 1) / c.G) : 0;
+  const int end = max(0, attn_limit(c, n, min(pt.tile * 256 + 255, a.R - 1) / c.G));
+  const int all = (end + 31) / 32, per = (all + a.splits - 1) / a.splits;
+  const int first = pt.split * per, T = max(0, min(all, first + per) - first);
+  const char* Kh = c.K.p + pt.b * c.K.b + pt.hk * c.K.h;
+  const char* Vh = c.V.p + pt.b * c.V.b + pt.hk * c.V.h;
+  uint32_t dk[DPW], dv[DPW];
+#pragma unroll
+  for (int x = 0; x < DPW; ++x) {
+    const int row = 4 * (wave * DPW + x) + lane / 16;
+    const uint32_t chunk = ((lane % 16) ^ bw_swizzle(row)) << 4;
+    dk[x] = row * (uint32_t)c.K.n + chunk;
+    dv[x] = row * (uint32_t)c.V.n + chunk;
+  }
+  const uint32_t lds0 = lds_address(lds) + wave * DPW * 1024;
+  bf16x8 qf[2][8], df[2][8];
+  int lim[2];
+  float lse[2], sum[2] = {0.f, 0.f};
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int r = min(row0 + 32 * u + lane % 32, a.R - 1), i = r / c.G, head = pt.hk * c.G + r % c.G;
+    lim[u] = attn_limit(c, n, i);
+    const char* q = c.Q.p + pt.b * c.Q.b + head * c.Q.h + i * c.Q.n + 16 * hh;
+    const char* o = c.O.p + pt.b * c.O.b + head * c.O.h + i * c.O.n + 16 * hh;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      qf[u][s] = *reinterpret_cast<const bf16x8*>(q + 32 * s);
+      df[u][s] = *reinterpret_cast<const bf16x8*>(o + 32 * s);
+    }
+    lse[u] = a.lse[((long)pt.b * a.H + head) * c.Nq + i];
+    if (lse[u] == -__builtin_inff()) lse[u] = __builtin_inff();
+  }
+  wait_vm<0>();
+
+  auto issue = [&](int t, int buf) {
+    const int k0 = (first + t) * 32;
+    const uint32_t dst = lds0 + buf * STAGE;
+    const char* kb = Kh + (long)k0 * c.K.n;
+    const char* vb = Vh + (long)k0 * c.V.n;
+#pragma unroll
+    for (int x = 0; x < DPW; ++x) {
+      uint32_t ok = dk[x], ov = dv[x];
+      if (k0 + 32 > n) {  // rows past the last key re-read it
+        const int back = max(4 * (wave * DPW + x) + lane / 16 - (n - 1 - k0), 0);
+        ok -= back * (uint32_t)c.K.n;
+        ov -= back * (uint32_t)c.V.n;
+      }
+      dma16(kb, ok, dst + x * 1024);
+      dma16(vb, ov, dst + kTile + x * 1024);
+    }
+  };
+  int issued = 0;
+#pragma unroll
+  for (int j = 0; j < NBUF - 1; ++j)
+    if (j < T) issue(j, j), ++issued;
+  for (int t = 0; t < T;) {
+#pragma unroll
+    for (int j = 0; j < NBUF; ++j) {
+      if (t >= T) break;
+      if (issued == t + NBUF - 1)
+        wait_vm<2 * DPW * (NBUF - 2)>();
+      else
+        __builtin_amdgcn_s_waitcnt(0);
+      __syncthreads();
+      if (issued < T) issue(issued, (j + NBUF - 1) % NBUF), ++issued;
+      const int k0 = (first + t) * 32;
+      if (k0 < lim_hi) {
+        const char* Kt = lds + j * STAGE;
+        f32x16 sc[2] = {f32x16{}, f32x16{}}, dp[2] = {f32x16{}, f32x16{}};
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+          const bf16x8 x = row_frag(Kt, lane % 32, s, hh), y = row_frag(Kt + kTile, lane % 32, s, hh);
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            sc[u] = mfma_bf16(x, qf[u][s], sc[u]);
+            dp[u] = mfma_bf16(y, df[u][s], dp[u]);
+          }
+        }
+        __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);  // DS reads
+#pragma unroll
+        for (int s = 0; s < 10; ++s) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);  // MFMA
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        if (k0 + 32 > lim_lo) {  // value k: key k0 + 8(k/4) + 4 hh + k%4 of this lane's rows
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const int left = lim[u] - k0 - 4 * hh;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) sc[u][k] = 8 * (k / 4) + k % 4 < left ? sc[u][k] : -__builtin_inff();
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int k = 0; k < 16; ++k)
+            sum[u] = fmaf(__builtin_amdgcn_exp2f(fmaf(sc[u][k], c.scale_log2, -lse[u])), dp[u][k], sum[u]);
+      }
+      ++t;
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int r = row0 + 32 * u + lane % 32;
+    const float s = halves_sum(sum[u]);
+    if (r < a.R && hh == 0) a.part[(pt.bh * a.splits + pt.split) * a.R + r] = s;
+  }
+}
+
 // Four waves of 32 rows walk the keys in sub-tiles of 32 through three LDS stages:
 //   S^T = K Q^T, dP^T = V dO^T (a lane has one row and 16 keys of it), dQ^T += K^T dS^T.
+// dS goes into its product as two bf16 terms, the rounded value and what that left: the sum over the keys
+// cancels, and one term's rounding alone would be 0.0019 to 0.0021 of dQ's norm beside dQ's own 0.0017.
 __global__ __launch_bounds__(256, 2) void attn_dq_bf16_kernel(const GradArgs a) {
   constexpr int STAGE = 2 * kTile, NBUF = 3, DPW = 2;
   __shared__ __attribute__((aligned(1024))) char lds[NBUF * STAGE];
@@ -150,7 +281,8 @@ __global__ __launch_bounds__(256, 2) void attn_dq_bf16_kernel(const GradArgs a) 
       df[s] = *reinterpret_cast<const bf16x8*>(o + 32 * s);
     }
   }
-  const float2 ld = a.lseD[((long)pt.b * c.Hkv * c.G + head) * a.Np + i];
+  const float* st = a.stat + stat_at((long)pt.b * a.H + head, a.Np, i);
+  const float lse = st[0], dsum = st[32];
   wait_vm<0>();
   f32x16 acc[4];
 #pragma unroll
@@ -219,22 +351,26 @@ __global__ __launch_bounds__(256, 2) void attn_dq_bf16_kernel(const GradArgs a) 
           for (int k = 0; k < 16; ++k) sc[k] = 8 * (k / 4) + k % 4 < left ? sc[k] : -__builtin_inff();
         }
         __builtin_amdgcn_sched_barrier(0);
-        bf16x8 ds[2];
+        bf16x8 ds[2], dl[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
-            const float p = __builtin_amdgcn_exp2f(fmaf(sc[8 * u + k], c.scale_log2, -ld.x));
-            ds[u][k] = (bf16)(p * (dp[8 * u + k] - ld.y));
+            const float p = __builtin_amdgcn_exp2f(fmaf(sc[8 * u + k], c.scale_log2, -lse));
+            const float x = p * (dp[8 * u + k] - dsum);
+            ds[u][k] = (bf16)x;
+            dl[u][k] = (bf16)(x - (float)ds[u][k]);
           }
 #pragma unroll
           for (int w = 0; w < 4; ++w) acc[w] = mfma_bf16(kt[4 * u + w], ds[u], acc[w]);
-        }
-        __builtin_amdgcn_sched_group_barrier(0x402, 36, 0);
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
+          for (int w = 0; w < 4; ++w) acc[w] = mfma_bf16(kt[4 * u + w], dl[u], acc[w]);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x402, 60, 0);
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
           __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x402, 9, 0);
+          __builtin_amdgcn_sched_group_barrier(0x402, 8, 0);
         }
       }
       ++t;
@@ -269,7 +405,8 @@ __global__ __launch_bounds__(256) void attn_dq_f32_kernel(const GradArgs a) {
   float4 qv[W], dv[W];
   f32_quarter<D>(c.Q.p + pt.b * c.Q.b + head * c.Q.h + i * c.Q.n, lane, qv);
   f32_quarter<D>(c.O.p + pt.b * c.O.b + head * c.O.h + i * c.O.n, lane, dv);
-  const float2 ld = a.lseD[((long)pt.b * c.Hkv * c.G + head) * a.Np + i];
+  const float* st = a.stat + stat_at((long)pt.b * a.H + head, a.Np, i);
+  const float lse = st[0], dsum = st[32];
   f32x4 acc[W];
 #pragma unroll
   for (int w = 0; w < W; ++w) acc[w] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -303,8 +440,8 @@ __global__ __launch_bounds__(256) void attn_dq_f32_kernel(const GradArgs a) {
       float ds[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float p = k0 + 4 * gr + k < lim ? __builtin_amdgcn_exp2f(fmaf(sc[k], c.scale_log2, -ld.x)) : 0.f;
-        ds[k] = p * (dp[k] - ld.y);
+        const float p = k0 + 4 * gr + k < lim ? __builtin_amdgcn_exp2f(fmaf(sc[k], c.scale_log2, -lse)) : 0.f;
+        ds[k] = p * (dp[k] - dsum);
       }
       f32_cols<D>(ks + 16 * u * LD, ds, acc, lane);
     }
@@ -334,161 +471,206 @@ __device__ __forceinline__ Walk walk_of(const GradArgs& a, int n, int key0, int 
   return w;
 }
 
-// bf16: a workgroup has 128 keys, in two roles of four waves over the same 32-key columns. Role 0 holds the
+// bf16: a workgroup has 128 keys, in two roles of two waves over the same 64-key columns. Role 0 holds the
 // keys' K: S = Q K^T, P, dV^T += dO^T P. Role 1 holds their V: dP = dO V^T, dS = P (dP - D), dK^T += Q^T dS, with
 // P from role 0 through LDS one step later, as fp16 (P lies in [0, 1], where that is an eighth of the
-// rounding to bf16 that dS takes next). A wave then has one operand set and one accumulator set, and two waves
-// run per SIMD. Operands are read from LDS a product ahead: the next step's rows during the second product,
-// the transposed ones during the first.
-constexpr int kDkvBuf = 4;
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2)))
-void attn_dkv_bf16_kernel(const GradArgs a) {
-  constexpr int NKW = 4, STAGE = 2 * kTile + 1024, DPW = 2, PBUF = NKW * 2048, NBUF = kDkvBuf;
-  constexpr int AHEAD = NBUF - 3;
-  static_assert(AHEAD == 1, "every load in flight is the next step's: the waits below are for all of them");
+// rounding to bf16 that dS takes next). A wave has its SIMD to itself: two 32-key tiles, so that what it reads
+// from LDS serves two products (one tile per wave and two waves per SIMD read 1.5 times what the LDS delivers
+// while the products run), and the softmax of one tile lies between the products of the other:
+//   S_0 | S_1 with P_0 | dV_0 with P_1 | dV_1 with the next step's row operand.
+constexpr int kDkvBuf = 5;
+template <bool CAUSAL>
+__global__ __launch_bounds__(256, 1) void attn_dkv_bf16_kernel(const GradArgs a) {
+  constexpr int STAGE = 2 * kTile + 1024, DPW = 4, PBUF = 4 * 2048, NBUF = kDkvBuf;
   __shared__ __attribute__((aligned(1024))) char lds[NBUF * STAGE + 2 * PBUF];
   const AttnCall& c = a.c;
   const Part pt = part_of(a, xcd_remap(blockIdx.x, a.total), false);
   const int lane = threadIdx.x % 64, hh = lane / 32;
-  const int wave = wave_uniform(threadIdx.x / 64), role = wave / NKW, kw = wave % NKW;
+  const int wave = wave_uniform(threadIdx.x / 64), role = wave / 2, kw = wave % 2;
   const int n = attn_keys(c, pt.b), off = n - c.Nq;
-  const int key0 = pt.tile * 128, key = key0 + kw * 32 + lane % 32;
+  const int key0 = pt.tile * 128, key = key0 + kw * 64 + lane % 32;  // and key + 32
   const Walk wk = walk_of(a, n, key0, pt.split);
   const int T = wk.t1 - wk.t0;
 
-  bf16x8 bf[8];
+  bf16x8 bf[2][8];
   {
-    const View& src = role ? c.V : c.K;
-    const char* row = src.p + pt.b * src.b + pt.hk * src.h + (long)max(0, min(key, n - 1)) * src.n + 16 * hh;
+    const char* base = role ? c.V.p + pt.b * c.V.b + pt.hk * c.V.h : c.K.p + pt.b * c.K.b + pt.hk * c.K.h;
+    const long nstride = role ? c.V.n : c.K.n;
 #pragma unroll
-    for (int s = 0; s < 8; ++s) bf[s] = *reinterpret_cast<const bf16x8*>(row + 32 * s);
+    for (int u = 0; u < 2; ++u) {
+      const char* row = base + (long)max(0, min(key + 32 * u, n - 1)) * nstride + 16 * hh;
+#pragma unroll
+      for (int s = 0; s < 8; ++s) bf[u][s] = *reinterpret_cast<const bf16x8*>(row + 32 * s);
+    }
   }
   wait_vm<0>();
-  f32x16 acc[4];
+  f32x16 acc[2][4];
 #pragma unroll
-  for (int w = 0; w < 4; ++w) acc[w] = f32x16{};
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int w = 0; w < 4; ++w) acc[u][w] = f32x16{};
 
-  // Loads of a step: waves 0-3 the Q rows, waves 4-7 the dO rows, 8 rows each.
-  const View& mine = wave < 4 ? c.Q : c.O;
+  // Loads of a step: waves 0 and 1 the Q rows, waves 2 and 3 the dO rows, 16 rows each.
+  const long nstride = role ? c.O.n : c.Q.n, hstride = role ? c.O.h : c.Q.h;
   uint32_t dsrc[DPW];
 #pragma unroll
   for (int x = 0; x < DPW; ++x) {
-    const int row = 4 * ((wave % 4) * DPW + x) + lane / 16;
-    dsrc[x] = row * (uint32_t)mine.n + (((lane % 16) ^ bw_swizzle(row)) << 4);
+    const int row = 4 * (kw * DPW + x) + lane / 16;
+    dsrc[x] = row * (uint32_t)nstride + (((lane % 16) ^ bw_swizzle(row)) << 4);
   }
   const uint32_t lds0 = lds_address(lds);
-  const uint32_t dst0 = lds0 + (wave / 4) * kTile + (wave % 4) * DPW * 1024;
-  const char* mbase = mine.p + pt.b * mine.b + (long)pt.hk * c.G * mine.h;
-  const char* lbase = reinterpret_cast<const char*>(a.lseD + ((long)pt.b * c.Hkv + pt.hk) * c.G * a.Np);
+  const uint32_t dst0 = lds0 + role * kTile + kw * DPW * 1024;
+  const char* mbase = (role ? c.O.p + pt.b * c.O.b : c.Q.p + pt.b * c.Q.b) + (long)pt.hk * c.G * hstride;
+  const char* sbase = reinterpret_cast<const char*>(a.stat + ((long)pt.b * a.H + (long)pt.hk * c.G) * a.Np * 2);
   int ig = 0, iq = wk.q0, cq = wk.q0;  // the next step to load; the query of the next step to take
   if (wk.tiles > 0) {
     ig = wk.t0 / wk.tiles;
     iq = cq = wk.q0 + wk.t0 % wk.tiles * 32;
   }
-  auto issue = [&](int buf) {
-    const char* base = mbase + ig * mine.h + (long)iq * mine.n;
-    const uint32_t dst = dst0 + buf * STAGE;
+  int issued = 0, ibuf = 0;
+  auto issue = [&]() {
+    const char* base = mbase + ig * hstride + (long)iq * nstride;
+    const uint32_t dst = dst0 + ibuf * STAGE;
+    if (iq + 32 <= c.Nq) {
 #pragma unroll
-    for (int x = 0; x < DPW; ++x) {
-      uint32_t o = dsrc[x];
-      if (iq + 32 > c.Nq)  // rows past the last query re-read it (P = 0 there)
-        o -= max(4 * ((wave % 4) * DPW + x) + lane / 16 - (c.Nq - 1 - iq), 0) * (uint32_t)mine.n;
-      dma16(base, o, dst + x * 1024);
+      for (int x = 0; x < DPW; ++x) dma16(base, dsrc[x], dst + x * 1024);
+    } else {  // rows past the last query re-read it (P = 0 there)
+#pragma unroll
+      for (int x = 0; x < DPW; ++x) {
+        const int back = max(4 * (kw * DPW + x) + lane / 16 - (c.Nq - 1 - iq), 0);
+        dma16(base, dsrc[x] - back * (uint32_t)nstride, dst + x * 1024);
+      }
     }
     // lse, D of the 32 queries (256 bytes; lanes 16-63 repeat lanes 0-15)
-    if (wave == 0)
-      dma16(lbase + ((long)ig * a.Np + iq) * 8, (lane % 16) * 16, lds0 + buf * STAGE + 2 * kTile);
+    if (wave == 0) dma16(sbase + ((long)ig * a.Np + iq) * 8, (lane % 16) * 16, lds0 + ibuf * STAGE + 2 * kTile);
     iq += 32;
     if (iq >= c.Nq) iq = wk.q0, ++ig;
+    ++issued;
+    if (++ibuf == NBUF) ibuf = 0;
   };
 
-  char* pbase = lds + NBUF * STAGE + kw * 2048 + lane * 16;  // + buffer * PBUF + u * 1024
-  int issued = 0;
+  char* pbase = lds + NBUF * STAGE + kw * 4096 + lane * 16;  // + buffer * PBUF + tile * 2048 + half * 1024
 #pragma unroll
-  for (int j = 0; j <= AHEAD; ++j)
-    if (j < T) issue(j), ++issued;
+  for (int j = 0; j < NBUF - 2; ++j)
+    if (j < T) issue();
   wait_vm<0>();
   __syncthreads();
-  // Iteration t: role 0 takes step t, role 1 step t - 1. Both meet the same barriers, in whole turns of NBUF.
+  // Iteration t: role 0 takes step t, role 1 step t - 1; the row operand of the step after is read in both. The
+  // loads of step t + NBUF - 2 go where role 1 was one iteration ago.
   auto walk = [&](auto role_tag) {
     constexpr int ROLE = decltype(role_tag)::value;
-    bf16x8 fa[8];  // row operands (Q for role 0, dO for role 1) of the wave's next step
-    auto row_operands = [&](int stage) {
+    bf16x8 fa[8];
+    auto row_operands = [&](const char* tile) {
 #pragma unroll
-      for (int s = 0; s < 8; ++s) fa[s] = row_frag(lds + stage * STAGE + ROLE * kTile, lane % 32, s, hh);
+      for (int s = 0; s < 8; ++s) fa[s] = row_frag(tile, lane % 32, s, hh);
     };
-    if (ROLE == 0) row_operands(0);
-    for (int t = 0; t <= T;) {
+    if (ROLE == 0) row_operands(lds);
+    int buf = 0, back = NBUF - 1;  // stages of steps t and t - 1
+    for (int t = 0; t <= T; ++t) {
+      if (issued >= t + 3)  // stage t + 1 has landed; one more step's loads may be under way
+        wait_vm<DPW>();
+      else
+        wait_vm<0>();
+      __syncthreads();
+      if (issued < T) issue();
+      const int ahead = buf + 1 == NBUF ? 0 : buf + 1;
+      if (ROLE == 0 ? t < T : t > 0) {
+        const char* stage = lds + (ROLE ? back : buf) * STAGE;
+        char* pb = pbase + ((t - ROLE) & 1) * PBUF;
+        bf16x8 fb[8];
+        float4 lv[4];  // lse (role 0) or D (role 1) of the step's queries 8 j + 4 hh ..
+        f16x8 ph[2][2];
+        f32x16 X[2] = {f32x16{}, f32x16{}};
+        bf16x8 b2[2][2];
+        // P or dS of tile u
+        auto middle = [&](int u) {
 #pragma unroll
-      for (int b = 0; b < NBUF; ++b, ++t) {
-        wait_vm<0>();  // stage t + 1 has landed
-        __syncthreads();
-        if (issued < T) issue((b + 1 + AHEAD) % NBUF), ++issued;
-        const int step = t - ROLE;
-        if (step >= 0 && step < T) {
-          const char* stage = lds + (ROLE ? (b + NBUF - 1) % NBUF : b) * STAGE;
-          const float* lt = reinterpret_cast<const float*>(stage + 2 * kTile) + ROLE;
-          char* pb = pbase + ((b + ROLE) % 2) * PBUF;  // role 0 writes step t's, role 1 reads t - 1's
-          bf16x8 fb[8];
-#pragma unroll
-          for (int w = 0; w < 4; ++w)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) fb[2 * w + u] = tr_frag(stage + (1 - ROLE) * kTile, w, u, lane);
-          float lv[16];  // lse (role 0) or D (role 1) of the step's queries
-#pragma unroll
-          for (int k = 0; k < 16; ++k) lv[k] = lt[2 * (8 * (k / 4) + 4 * hh + k % 4)];
-          // S (role 0) or dP (role 1): one lane per key; rows 8j + 4(l/32) + e are the step's queries
-          f32x16 X = f32x16{};
-#pragma unroll
-          for (int s = 0; s < 8; ++s) X = mfma_bf16(fa[s], bf[s], X);
-          f16x8 ph[2];
-          if constexpr (ROLE == 1) {
-            ph[0] = *reinterpret_cast<const f16x8*>(pb);
-            ph[1] = *reinterpret_cast<const f16x8*>(pb + 1024);
+          for (int k = 0; k < 16; ++k) {
+            const float v = k % 4 == 0 ? lv[k / 4].x : k % 4 == 1 ? lv[k / 4].y : k % 4 == 2 ? lv[k / 4].z : lv[k / 4].w;
+            if constexpr (ROLE == 0) {
+              const float p = __builtin_amdgcn_exp2f(fmaf(X[u][k], c.scale_log2, -v));
+              b2[u][k / 8][k % 8] = (bf16)p;
+              ph[u][k / 8][k % 8] = (_Float16)p;
+            } else {
+              b2[u][k / 8][k % 8] = (bf16)((float)ph[u][k / 8][k % 8] * (X[u][k] - v));
+            }
           }
-          __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
-#pragma unroll
-          for (int s = 0; s < 8; ++s) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+          if constexpr (ROLE == 0) {
+            *reinterpret_cast<f16x8*>(pb + u * 2048) = ph[u][0];
+            *reinterpret_cast<f16x8*>(pb + u * 2048 + 1024) = ph[u][1];
           }
-          __builtin_amdgcn_sched_barrier(0);
-          row_operands(ROLE ? b : (b + 1) % NBUF);
-          if (ROLE == 0 && c.causal && key0 + 127 > cq + off) {  // P = 0 where the query is before the key
-            const int late = key - off - cq - 4 * hh;
+        };
+        auto hide = [&](int u) {  // P = 0 where the query is before the key
+          if (CAUSAL && ROLE == 0 && key0 + kw * 64 + 32 * u + 31 > cq + off) {
+            const int late = key + 32 * u - off - cq - 4 * hh;
 #pragma unroll
-            for (int k = 0; k < 16; ++k) lv[k] = 8 * (k / 4) + k % 4 >= late ? lv[k] : __builtin_inff();
+            for (int k = 0; k < 16; ++k) X[u][k] = 8 * (k / 4) + k % 4 >= late ? X[u][k] : -__builtin_inff();
           }
-          cq += 32;
-          if (cq >= c.Nq) cq = wk.q0;
-          __builtin_amdgcn_sched_barrier(0);
-          bf16x8 b2[2];
+        };
+#pragma unroll
+        for (int s = 0; s < 8; ++s) X[0] = mfma_bf16(fa[s], bf[0][s], X[0]);
+        if constexpr (ROLE == 1) {
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              if constexpr (ROLE == 0) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(X[8 * u + k], c.scale_log2, -lv[8 * u + k]));
-                b2[u][k] = (bf16)p;
-                ph[u][k] = (_Float16)p;
-              } else {
-                b2[u][k] = (bf16)((float)ph[u][k] * (X[8 * u + k] - lv[8 * u + k]));
-              }
-            }
-            if constexpr (ROLE == 0) *reinterpret_cast<f16x8*>(pb + 1024 * u) = ph[u];
-#pragma unroll
-            for (int w = 0; w < 4; ++w) acc[w] = mfma_bf16(fb[2 * w + u], b2[u], acc[w]);
+            ph[u][0] = *reinterpret_cast<const f16x8*>(pb + u * 2048);
+            ph[u][1] = *reinterpret_cast<const f16x8*>(pb + u * 2048 + 1024);
           }
-          __builtin_amdgcn_sched_group_barrier(0x402, 28, 0);
-#pragma unroll
-          for (int s = 0; s < 4; ++s) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x402, 7, 0);
-          }
-        } else if (step < 0) {
-          row_operands(0);
         }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          lv[j] = *reinterpret_cast<const float4*>(stage + 2 * kTile + ROLE * 128 + 32 * j + 16 * hh);
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+#pragma unroll
+          for (int v = 0; v < 2; ++v) fb[2 * w + v] = tr_frag(stage + (1 - ROLE) * kTile, w, v, lane);
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // MFMA
+          __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);  // DS reads
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        hide(0);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int s = 0; s < 8; ++s) X[1] = mfma_bf16(fa[s], bf[1][s], X[1]);
+        middle(0);
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x402, 8, 0);  // VALU, transcendentals
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        hide(1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int v = 0; v < 2; ++v)
+#pragma unroll
+          for (int w = 0; w < 4; ++w) acc[0][w] = mfma_bf16(fb[2 * w + v], b2[0][v], acc[0][w]);
+        middle(1);
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x402, 8, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        row_operands(lds + (ROLE ? buf : ahead) * STAGE + ROLE * kTile);
+#pragma unroll
+        for (int v = 0; v < 2; ++v)
+#pragma unroll
+          for (int w = 0; w < 4; ++w) acc[1][w] = mfma_bf16(fb[2 * w + v], b2[1][v], acc[1][w]);
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        cq += 32;
+        if (cq >= c.Nq) cq = wk.q0;
+      } else if (ROLE == 1 && t == 0) {
+        row_operands(lds + kTile);
       }
+      back = buf;
+      buf = ahead;
     }
   };
   if (T > 0) {
@@ -497,18 +679,22 @@ void attn_dkv_bf16_kernel(const GradArgs a) {
     else
       walk(std::integral_constant<int, 0>{});
   }
-  if (key >= c.Nk) return;
-  if (key >= n) {  // a key that is not there (its column holds the last one's)
 #pragma unroll
-    for (int w = 0; w < 4; ++w) acc[w] = f32x16{};
-  }
-  const float f = role ? c.scale : 1.f;
-  if (a.splits > 1) {
-    float* out = a.part + (role ? 0 : a.part2) + ((pt.bh * a.splits + pt.split) * c.Nk + key) * 128;
-    store_grad_row<false>(out, acc, f, hh, nullptr, nullptr);
-  } else {
-    const View& g = role ? a.G1 : a.G2;
-    store_row_bf16(g.p + pt.b * g.b + pt.hk * g.h + key * g.n, acc, f, hh);
+  for (int u = 0; u < 2; ++u) {
+    const int k = key + 32 * u;
+    if (k >= c.Nk) break;
+    if (k >= n) {  // a key that is not there (its column holds the last one's)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) acc[u][w] = f32x16{};
+    }
+    const float f = role ? c.scale : 1.f;
+    if (a.splits > 1) {
+      float* out = a.part + (role ? 0 : a.part2) + ((pt.bh * a.splits + pt.split) * c.Nk + k) * 128;
+      store_grad_row<false>(out, acc[u], f, hh, nullptr, nullptr);
+    } else {
+      const View& g = role ? a.G1 : a.G2;
+      store_row_bf16(g.p + pt.b * g.b + pt.hk * g.h + k * g.n, acc[u], f, hh);
+    }
   }
 }
 
@@ -517,7 +703,7 @@ template <int D>
 __global__ __launch_bounds__(256) void attn_dkv_f32_kernel(const GradArgs a) {
   constexpr int W = D / 16, LD = D + 4, PT = 32 * D / 4 / 256;
   __shared__ __attribute__((aligned(16))) float qs[32 * LD], os[32 * LD];
-  __shared__ float2 st[32];
+  __shared__ float st[64];
   const AttnCall& c = a.c;
   const Part pt = part_of(a, xcd_remap(blockIdx.x, a.total), false);
   const int wave = wave_uniform(threadIdx.x / 64), lane = threadIdx.x % 64, gr = lane / 16;
@@ -534,7 +720,7 @@ __global__ __launch_bounds__(256) void attn_dkv_f32_kernel(const GradArgs a) {
 #pragma unroll
   for (int w = 0; w < W; ++w) dk[w] = dv[w] = f32x4{0.f, 0.f, 0.f, 0.f};
   float4 qn[PT], on[PT];
-  float2 sn = make_float2(0.f, 0.f);
+  float sn = 0.f;
   int g = 0, q = wk.q0;
   if (wk.tiles > 0) {
     g = wk.t0 / wk.tiles;
@@ -551,7 +737,7 @@ __global__ __launch_bounds__(256) void attn_dkv_f32_kernel(const GradArgs a) {
       qn[x] = reinterpret_cast<const float4*>(Qh + i * c.Q.n)[at];
       on[x] = reinterpret_cast<const float4*>(Oh + i * c.O.n)[at];
     }
-    if (threadIdx.x < 32) sn = a.lseD[((long)pt.b * c.Hkv * c.G + head) * a.Np + q + threadIdx.x];
+    if (threadIdx.x < 64) sn = a.stat[stat_at((long)pt.b * a.H + head, a.Np, q) + threadIdx.x];
   };
   if (wk.t0 < wk.t1) fetch();
   for (int t = wk.t0; t < wk.t1; ++t) {
@@ -562,7 +748,7 @@ __global__ __launch_bounds__(256) void attn_dkv_f32_kernel(const GradArgs a) {
       *reinterpret_cast<float4*>(qs + row * LD + 4 * at) = qn[x];
       *reinterpret_cast<float4*>(os + row * LD + 4 * at) = on[x];
     }
-    if (threadIdx.x < 32) st[threadIdx.x] = sn;
+    if (threadIdx.x < 64) st[threadIdx.x] = sn;
     __syncthreads();
     const int q0 = q;
     q += 32;
@@ -576,10 +762,9 @@ __global__ __launch_bounds__(256) void attn_dkv_f32_kernel(const GradArgs a) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {  // query q0 + 16 u + 4 gr + k
         const int row = 16 * u + 4 * gr + k;
-        const float2 s = st[row];
         const bool seen = !c.causal || key <= q0 + row + off;
-        p[k] = seen ? __builtin_amdgcn_exp2f(fmaf(sc[k], c.scale_log2, -s.x)) : 0.f;
-        ds[k] = p[k] * (dp[k] - s.y);
+        p[k] = seen ? __builtin_amdgcn_exp2f(fmaf(sc[k], c.scale_log2, -st[row])) : 0.f;
+        ds[k] = p[k] * (dp[k] - st[32 + row]);
       }
       f32_cols<D>(os + 16 * u * LD, p, dv, lane);
       f32_cols<D>(qs + 16 * u * LD, ds, dk, lane);
@@ -624,8 +809,8 @@ __global__ __launch_bounds__(256) void attn_sum_kernel(int Hkv, int G, int rows,
 
 struct GradPlan {
   int R, Np;
-  int qtiles, qsplits, ktiles, ksplits;
-  size_t lsed, qpart, kpart;  // bytes, 256-aligned; kpart: of dK, and as many of dV
+  int qtiles, qsplits, ktiles, ksplits, dtiles, dsplits;
+  size_t stat, qpart, kpart, dpart;  // bytes, 256-aligned; kpart: of dK, and as many of dV
 };
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 GradPlan grad_plan(const AttnShape& s) {
@@ -641,7 +826,10 @@ GradPlan grad_plan(const AttnShape& s) {
   const long qhold = 2 * kCus, khold = (s.bf16 ? 1 : 2) * kCus;
   p.qsplits = (int)std::max<long>(1, std::min<long>({qhold / (p.qtiles * bh), (s.Nk + 255) / 256, 64}));
   p.ksplits = (int)std::max<long>(1, std::min<long>({khold / (p.ktiles * bh), ((long)p.R + 511) / 512, 64}));
-  p.lsed = up256((size_t)s.B * s.H * p.Np * sizeof(float2));
+  p.dtiles = (p.R + 255) / 256;
+  p.dsplits = (int)std::max<long>(1, std::min<long>({qhold / (p.dtiles * bh), (s.Nk + 255) / 256, 64}));
+  p.stat = up256((size_t)s.B * s.H * p.Np * 2 * sizeof(float));
+  p.dpart = s.bf16 ? up256((size_t)bh * p.dsplits * p.R * sizeof(float)) : 0;
   p.qpart = p.qsplits > 1 ? up256((size_t)bh * p.qsplits * p.R * s.d * 4) : 0;
   p.kpart = p.ksplits > 1 ? up256((size_t)bh * p.ksplits * s.Nk * s.d * 4) : 0;
   return p;
@@ -661,7 +849,7 @@ hipError_t launch_sum(const AttnShape& s, int G, int rows, int splits, const flo
 
 size_t attn_backward_workspace_bytes(const AttnShape& s) {
   const GradPlan p = grad_plan(s);
-  return p.lsed + std::max(p.qpart, 2 * p.kpart);
+  return p.stat + std::max({p.dpart, p.qpart, 2 * p.kpart});
 }
 
 hipError_t launch_attn_backward(const AttnShape& s, const HeadView& Q, const HeadView& K, const HeadView& V,
@@ -671,19 +859,25 @@ hipError_t launch_attn_backward(const AttnShape& s, const HeadView& Q, const Hea
   const GradPlan p = grad_plan(s);
   GradArgs a{};
   a.c = attn_call(s, Q, K, V, dO, kv_len, scale);
-  a.R = p.R, a.Np = p.Np;
-  float2* lseD = (float2*)ws;
-  a.lseD = lseD;
-  a.part = (float*)((char*)ws + p.lsed);
+  a.R = p.R, a.Np = p.Np, a.H = s.H;
+  float* stat = (float*)ws;
+  a.stat = stat;
+  a.lse = lse;
+  a.part = (float*)((char*)ws + p.stat);
   const long rows = (long)s.B * s.H * p.Np;
-  const dim3 rgrid((unsigned)((rows * 16 + 255) / 256));
-  if (s.bf16)
-    hipLaunchKernelGGL(attn_rowdot_bf16_kernel, rgrid, dim3(256), 0, st, s.H, s.Nq, p.Np, rows,
-                       view_of(O, true), a.c.O, lse, lseD);
-  else
-    hipLaunchKernelGGL(attn_rowdot_f32_kernel, rgrid, dim3(256), 0, st, s.H, s.Nq, p.Np, s.d, rows,
-                       view_of(O, false), a.c.O, lse, lseD);
-  hipError_t e = hipGetLastError();
+  hipError_t e;
+  if (s.bf16) {
+    a.tiles = p.dtiles, a.splits = p.dsplits, a.total = s.B * s.Hkv * p.dtiles * p.dsplits;
+    hipLaunchKernelGGL(attn_rowsum_bf16_kernel, dim3(a.total), dim3(256), 0, st, a);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(attn_stat_kernel, dim3((unsigned)((rows + 255) / 256)), dim3(256), 0, st, s.H, s.H / s.Hkv,
+                       s.Nq, p.Np, p.dsplits, rows, lse, (const float*)a.part, stat);
+  } else {
+    hipLaunchKernelGGL(attn_rowdot_f32_kernel, dim3((unsigned)((rows * 16 + 255) / 256)), dim3(256), 0, st, s.H,
+                       s.Nq, p.Np, s.d, rows, view_of(O, false), a.c.O, lse, stat);
+  }
+  e = hipGetLastError();
   if (e != hipSuccess) return e;
   const long bh = (long)s.B * s.Hkv;
   a.G1 = view_of(dQ, s.bf16);
@@ -698,7 +892,8 @@ hipError_t launch_attn_backward(const AttnShape& s, const HeadView& Q, const Hea
   a.tiles = p.ktiles, a.splits = p.ksplits, a.total = (int)(bh * p.ktiles * p.ksplits);
   a.part2 = (long)(p.kpart / sizeof(float));
   if (s.bf16)
-    hipLaunchKernelGGL(attn_dkv_bf16_kernel, dim3(a.total), dim3(512), 0, st, a);
+    hipLaunchKernelGGL(s.causal ? attn_dkv_bf16_kernel<true> : attn_dkv_bf16_kernel<false>, dim3(a.total), dim3(256),
+                       0, st, a);
   else
     hipLaunchKernelGGL(s.d == 64 ? attn_dkv_f32_kernel<64> : attn_dkv_f32_kernel<128>, dim3(a.total), dim3(256),
                        0, st, a);

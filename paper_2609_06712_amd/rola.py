@@ -961,8 +961,8 @@ def _norm_key(x, w, groups, kind):
 
 def rola_norm(X, W=None, Bias=None, kind="layer", eps=1e-6, out=None, want_stats=False, stream=None):
     """Layer norm ("layer") or RMS norm ("rms") of X [rows, d] or [B, N, d] (rows at one stride) with
-    W and Bias [d], or [B, d] for a weight per sample; either may be None. Returns Y, or with want_stats
-    (Y, mean, rstd), the fp32 statistics per row that rola_norm_backward takes (mean None for "rms")."""
+    W and Bias [d], or [B, d] for a weight per sample; either may be None. Returns (Y, mean, rstd): with
+    want_stats the fp32 statistics per row that rola_norm_backward takes (mean None for "rms"), else None."""
     if kind not in NORM_KIND:
         raise ValueError(f"kind must be one of {sorted(NORM_KIND)}, got {kind!r}")
     a = _Args()
@@ -986,7 +986,7 @@ def rola_norm(X, W=None, Bias=None, kind="layer", eps=1e-6, out=None, want_stats
     prob = _norm_problem(*_norm_key(X, Bias if W is None else W, groups, kind))
     _check(LIB.rola_norm(prob, _ptr(X), ldx, _ptr(W), _ptr(Bias), eps, _ptr(out), ldy, _ptr(mean), _ptr(rstd),
                          _stream(stream)), "rola_norm")
-    return (out, mean, rstd) if want_stats else out
+    return out, mean, rstd
 
 
 def norm_backward_workspace_bytes(X, W=None, kind="layer") -> int:
