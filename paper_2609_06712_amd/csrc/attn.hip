@@ -13,8 +13,8 @@
 //   QW = 4: four waves of 32 rows each walk the keys together, three LDS stages, three workgroups per CU.
 //   QW = 1: few rows (R <= 32): the four waves take every fourth sub-tile of the same rows through stages of
 //           their own, without barriers, and add up through LDS.
-// When the tiles of rows are too few for the chip, each is given to several workgroups that take a part of
-// the keys; their partial results (fp32, with maximum and sum) are joined by attn_join_kernel in a fixed order.
+// The tiles of rows that do not fill a round of the chip are cut over their keys (Cut); the partial results (fp32,
+// with maximum and sum) are joined by attn_join_kernel in a fixed order.
 //
 // fp32 (d 64, 128), on fp32 matrix instructions (attn_common.h): workgroups of 64 rows, 16 per wave.
 #include <algorithm>
@@ -30,27 +30,26 @@ constexpr int kTile = kKeys * 256;  // bytes of K or V of a sub-tile (bf16)
 
 struct FwdArgs {
   AttnCall c;
-  int tiles, splits, total, R;
+  Cut cut;
+  int R, rows;     // rows per key head, and per tile
   long heads;      // query heads, H
   float* lse;      // [B, H, Nq] or null
-  float* part;     // splits > 1: O [B Hkv][splits][R][d], then {max, sum} [B Hkv][splits][R]
+  float* part;     // of the cut tiles: O [left][splits][rows][d], and {max, sum} [left][splits][rows]
   float2* ml;
 };
 
-// The part of a tile's work that a workgroup has: sub-tiles [t0, t1) of `keys` keys, of (b, hk).
-struct Part {
-  int tile, split, b, hk;
-  long bh;
-};
-__device__ __forceinline__ Part part_of(const FwdArgs& a, int L) {
-  Part p;
-  const int t = L % a.tiles, rest = L / a.tiles;
-  p.tile = a.c.causal ? a.tiles - 1 - t : t;  // the longest walks first
-  p.split = rest % a.splits;
-  p.bh = rest / a.splits;
-  p.b = (int)(p.bh / a.c.Hkv);
-  p.hk = (int)(p.bh % a.c.Hkv);
-  return p;
+// V^T operand of a row-major [key][128] tile whose 16-byte chunks are swizzled by v_swizzle: as tr_frag, with
+// one address per channel tile for both halves of a k-step (four registers less than bw_swizzle takes).
+__device__ __forceinline__ int v_swizzle(int row) { return 2 * ((0x6530 >> (4 * (row & 3))) & 15); }
+__device__ __forceinline__ int v_offset(int w, int lane) {
+  const int i16 = lane % 16, row = 4 * (lane / 32) + i16 / 4, c = 2 * ((lane / 16) & 1) + ((i16 & 3) >> 1);
+  return row * 256 + (((4 * w + c) ^ v_swizzle(row)) << 4) + 8 * (i16 & 1);
+}
+__device__ __forceinline__ bf16x8 v_frag(const char* tile, int off, int u) {
+  const char* p = tile + off + 16 * u * 256;
+  const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)p);
+  const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(p + 8 * 256));
+  return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
 template <int QW>
@@ -61,7 +60,7 @@ __global__ __launch_bounds__(256, QW == 4 ? 3 : 1) void attn_bf16_kernel(const F
   constexpr int STEP = QW == 4 ? 1 : 4;        // sub-tiles between two of a wave's
   __shared__ __attribute__((aligned(1024))) char lds[(QW == 4 ? 1 : 4) * NBUF * STAGE];
   const AttnCall& c = a.c;
-  const Part pt = part_of(a, xcd_remap(blockIdx.x, a.total));
+  const Part pt = part_of(a.cut, c.Hkv, blockIdx.x, true);
   const int wave = wave_uniform(threadIdx.x / 64), lane = threadIdx.x % 64, hh = lane / 32;
   const int n = attn_keys(c, pt.b);
   const int row0 = (pt.tile * QW + (QW == 4 ? wave : 0)) * 32;  // first row of this wave
@@ -72,7 +71,7 @@ __global__ __launch_bounds__(256, QW == 4 ? 3 : 1) void attn_bf16_kernel(const F
   const int lim_lo = attn_limit(c, n, min(row0, a.R - 1) / c.G);
   const int lim_hi = row0 < a.R ? attn_limit(c, n, min(row0 + 31, a.R - 1) / c.G) : 0;
   const int end = max(0, attn_limit(c, n, min((pt.tile + 1) * 32 * QW - 1, a.R - 1) / c.G));
-  const int all = (end + kKeys - 1) / kKeys, per = (all + a.splits - 1) / a.splits;
+  const int all = (end + kKeys - 1) / kKeys, per = (all + pt.splits - 1) / pt.splits;
   const int t0 = pt.split * per, t1 = min(all, t0 + per);
   const int first = t0 + (QW == 4 ? 0 : wave);
   const int T = t1 > first ? (t1 - first + STEP - 1) / STEP : 0;  // this wave's sub-tiles
@@ -84,9 +83,8 @@ __global__ __launch_bounds__(256, QW == 4 ? 3 : 1) void attn_bf16_kernel(const F
 #pragma unroll
   for (int x = 0; x < DPW; ++x) {
     const int row = 4 * ((QW == 4 ? wave * DPW : 0) + x) + lane / 16;
-    const uint32_t chunk = ((lane % 16) ^ bw_swizzle(row)) << 4;
-    dk[x] = row * (uint32_t)c.K.n + chunk;
-    dv[x] = row * (uint32_t)c.V.n + chunk;
+    dk[x] = row * (uint32_t)c.K.n + (((lane % 16) ^ bw_swizzle(row)) << 4);
+    dv[x] = row * (uint32_t)c.V.n + (((lane % 16) ^ v_swizzle(row)) << 4);
   }
   const uint32_t lds0 = lds_address(lds) + (QW == 4 ? 0 : wave * NBUF * STAGE);
   char* stages = lds + (QW == 4 ? 0 : wave * NBUF * STAGE);
@@ -99,9 +97,10 @@ __global__ __launch_bounds__(256, QW == 4 ? 3 : 1) void attn_bf16_kernel(const F
   }
   wait_vm<0>();
 
+  int vo[4];
   f32x16 acc[4];
 #pragma unroll
-  for (int w = 0; w < 4; ++w) acc[w] = f32x16{};
+  for (int w = 0; w < 4; ++w) acc[w] = f32x16{}, vo[w] = v_offset(w, lane);
   float m = kNoMax, l = 0.f;
 
   auto issue = [&](int t, int buf) {  // sub-tile `t` of the wave's walk
@@ -158,7 +157,7 @@ __global__ __launch_bounds__(256, QW == 4 ? 3 : 1) void attn_bf16_kernel(const F
         }
         __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) vf[w] = tr_frag(Vt, w, 0, lane);
+        for (int w = 0; w < 4; ++w) vf[w] = v_frag(Vt, vo[w], 0);
         if (k0 + kKeys > lim_lo) {  // value k: key k0 + 8(k/4) + 4 hh + k%4 of this lane's row
           const int left = lim - k0 - 4 * hh;
 #pragma unroll
@@ -187,7 +186,7 @@ __global__ __launch_bounds__(256, QW == 4 ? 3 : 1) void attn_bf16_kernel(const F
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           acc[w] = mfma_bf16(vf[w], pb[0], acc[w]);
-          vf[w] = tr_frag(Vt, w, 1, lane);
+          vf[w] = v_frag(Vt, vo[w], 1);
         }
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
@@ -229,8 +228,8 @@ __global__ __launch_bounds__(256, QW == 4 ? 3 : 1) void attn_bf16_kernel(const F
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[e] = fmaf(f, os[(w * 32 + row) * 132 + c0 + e], o[e]);
     }
-    if (a.splits > 1) {
-      const long at = (pt.bh * a.splits + pt.split) * a.R + rr;
+    if (pt.left >= 0) {
+      const long at = ((long)pt.left * pt.splits + pt.split) * 32 + row;
       store8(a.part + at * D + c0, o);
       store8(a.part + at * D + c0 + 8, o + 8);
       if (c0 == 0) a.ml[at] = make_float2(mx, sum);
@@ -246,8 +245,8 @@ __global__ __launch_bounds__(256, QW == 4 ? 3 : 1) void attn_bf16_kernel(const F
     if (a.lse && c0 == 0)
       a.lse[(pt.b * a.heads + head) * c.Nq + ii] = sum > 0.f ? mx + __log2f(sum) : -__builtin_inff();
   } else if (rvalid) {
-    if (a.splits > 1) {
-      const long at = (pt.bh * a.splits + pt.split) * a.R + r;
+    if (pt.left >= 0) {
+      const long at = ((long)pt.left * pt.splits + pt.split) * 128 + wave * 32 + lane % 32;
       store_grad_row<false>(a.part + at * D, acc, 1.f, hh, nullptr, nullptr);
       if (hh == 0) a.ml[at] = make_float2(m, l);
       return;
@@ -275,7 +274,7 @@ __global__ __launch_bounds__(256) void attn_f32x_kernel(const FwdArgs a) {
   constexpr int W = D / 16, LD = D + 4, PT = 32 * D / 4 / 256;  // 16-byte pieces per thread, tensor and tile
   __shared__ __attribute__((aligned(16))) float ks[32 * LD], vs[32 * LD];
   const AttnCall& c = a.c;
-  const Part pt = part_of(a, xcd_remap(blockIdx.x, a.total));
+  const Part pt = part_of(a.cut, c.Hkv, blockIdx.x, true);
   const int wave = wave_uniform(threadIdx.x / 64), lane = threadIdx.x % 64, gr = lane / 16;
   const int n = attn_keys(c, pt.b);
   const int row0 = pt.tile * 64 + wave * 16;
@@ -284,7 +283,7 @@ __global__ __launch_bounds__(256) void attn_f32x_kernel(const FwdArgs a) {
   const int lim_lo = attn_limit(c, n, min(row0, a.R - 1) / c.G);
   const int lim_hi = row0 < a.R ? attn_limit(c, n, min(row0 + 15, a.R - 1) / c.G) : 0;
   const int end = max(0, attn_limit(c, n, min(pt.tile * 64 + 63, a.R - 1) / c.G));
-  const int all = (end + 31) / 32, per = (all + a.splits - 1) / a.splits;
+  const int all = (end + 31) / 32, per = (all + pt.splits - 1) / pt.splits;
   const int t0 = pt.split * per, t1 = min(all, t0 + per);
   const char* Kh = c.K.p + pt.b * c.K.b + pt.hk * c.K.h;
   const char* Vh = c.V.p + pt.b * c.V.b + pt.hk * c.V.h;
@@ -342,8 +341,8 @@ __global__ __launch_bounds__(256) void attn_f32x_kernel(const FwdArgs a) {
   }
   l = rows_sum(l);
   if (row0 + lane % 16 >= a.R) return;
-  if (a.splits > 1) {
-    const long at = (pt.bh * a.splits + pt.split) * a.R + r;
+  if (pt.left >= 0) {
+    const long at = ((long)pt.left * pt.splits + pt.split) * 64 + wave * 16 + lane % 16;
     f32_store<D>(reinterpret_cast<char*>(a.part + at * D), acc, 1.f, lane);
     if (gr == 0) a.ml[at] = make_float2(m, l);
     return;
@@ -354,28 +353,32 @@ __global__ __launch_bounds__(256) void attn_f32x_kernel(const FwdArgs a) {
     a.lse[(pt.b * a.heads + head) * c.Nq + i] = l > 0.f ? m + __log2f(l) : -__builtin_inff();
 }
 
-// Joins the parts of a row: a wave per row, D / 64 channels per lane.
+// Joins the parts of a cut tile's rows: a wave per row, D / 64 channels per lane.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void attn_join_kernel(const FwdArgs a, long rows) {
+__global__ __launch_bounds__(256) void attn_join_kernel(const FwdArgs a) {
   constexpr int V = D / 64;
-  const long at = (long)blockIdx.x * 4 + threadIdx.x / 64;  // (b, hk, row)
-  const int lane = threadIdx.x % 64;
-  if (at >= rows) return;
-  const long bh = at / a.R;
-  const int r = (int)(at % a.R);
-  const float2* ml = a.ml + bh * a.splits * a.R + r;
-  const float* part = a.part + (bh * a.splits * a.R + r) * D + lane * V;
+  const AttnCall& c = a.c;
+  const long at = (long)blockIdx.x * 4 + threadIdx.x / 64;  // (cut tile, row): rows is a multiple of 4
+  const int lane = threadIdx.x % 64, S = a.cut.splits;
+  const long left = at / a.rows;
+  const int row = (int)(at % a.rows);
+  int tile;
+  long bh;
+  cut_tile(a.cut, a.cut.whole + (int)left, true, &tile, &bh);
+  const int r = tile * a.rows + row;
+  if (r >= a.R) return;
+  const float2* ml = a.ml + left * S * a.rows + row;
+  const float* part = a.part + (left * S * a.rows + row) * D + lane * V;
   float mx = kNoMax;
-  for (int s = 0; s < a.splits; ++s) mx = fmaxf(mx, ml[(long)s * a.R].x);
+  for (int s = 0; s < S; ++s) mx = fmaxf(mx, ml[(long)s * a.rows].x);
   float sum = 0.f, o[V] = {};
-  for (int s = 0; s < a.splits; ++s) {
-    const float2 v = ml[(long)s * a.R];
+  for (int s = 0; s < S; ++s) {
+    const float2 v = ml[(long)s * a.rows];
     const float f = __builtin_amdgcn_exp2f(v.x - mx);
     sum = fmaf(f, v.y, sum);
 #pragma unroll
-    for (int k = 0; k < V; ++k) o[k] = fmaf(f, part[(long)s * a.R * D + k], o[k]);
+    for (int k = 0; k < V; ++k) o[k] = fmaf(f, part[(long)s * a.rows * D + k], o[k]);
   }
-  const AttnCall& c = a.c;
   const int b = (int)(bh / c.Hkv), i = r / c.G, head = (int)(bh % c.Hkv) * c.G + r % c.G;
   const float f = sum > 0.f ? 1.f / sum : 0.f;
   T* out = reinterpret_cast<T*>(c.O.p + b * c.O.b + head * c.O.h + i * c.O.n) + lane * V;
@@ -385,31 +388,26 @@ __global__ __launch_bounds__(256) void attn_join_kernel(const FwdArgs a, long ro
     a.lse[(b * a.heads + head) * c.Nq + i] = sum > 0.f ? mx + __log2f(sum) : -__builtin_inff();
 }
 
-// How a call is cut: rows per workgroup, and parts of the keys per tile of rows.
+// How a call is cut: rows per tile, and the parts of the tiles.
 struct FwdPlan {
-  int qw, tiles, splits;
-  long total;
+  int rows;
+  Cut cut;
 };
 FwdPlan fwd_plan(const AttnShape& s) {
-  const int R = s.Nq * (s.H / s.Hkv);
-  const bool few = s.bf16 && R <= 32;
-  const int rows = !s.bf16 ? 64 : few ? 32 : 128;
-  const int tiles = (R + rows - 1) / rows;
-  const long wgs = (long)tiles * s.B * s.Hkv;
-  // one round of the workgroups that the chip holds, each with at least `least` keys
-  const long hold = (few ? 4 : s.bf16 ? 3 : 4) * kCus;
-  const int least = few ? 512 : 256;
-  long splits = std::min<long>(std::max<long>(1, hold / wgs), (s.Nk + least - 1) / least);
-  splits = std::min<long>(splits, 64);
-  return {few ? 1 : 4, tiles, (int)splits, wgs * splits};
+  const int R = s.Nq * (s.H / s.Hkv), bh = s.B * s.Hkv, steps = (s.Nk + 31) / 32;
+  const int rows = !s.bf16 ? 64 : R <= 32 ? 32 : 128, tiles = (R + rows - 1) / rows;
+  const double bytes = rows * (s.d + 2) * 4.0;
+  // few rows: bound by reading K and V, in parts of a quarter round, which also evens out samples of different
+  // lengths
+  if (s.bf16 && R <= 32) return {rows, make_cut(tiles, bh, false, 4 * kCus, steps, 0.4, bytes, 16)};
+  return {rows, make_cut(tiles, bh, s.causal, s.bf16 ? 3 * kCus : 4 * kCus, steps, s.bf16 ? 0.9 : 2.0, bytes, 8)};
 }
 
 }  // namespace
 
 size_t attn_workspace_bytes(const AttnShape& s) {
   const FwdPlan p = fwd_plan(s);
-  if (p.splits == 1) return 0;
-  return (size_t)s.B * s.H * s.Nq * p.splits * (s.d + 2) * sizeof(float);
+  return (size_t)cut_left(p.cut) * p.cut.splits * p.rows * (s.d + 2) * sizeof(float);
 }
 
 hipError_t launch_attn(const AttnShape& s, const HeadView& Q, const HeadView& K, const HeadView& V,
@@ -418,21 +416,22 @@ hipError_t launch_attn(const AttnShape& s, const HeadView& Q, const HeadView& K,
   const FwdPlan p = fwd_plan(s);
   FwdArgs a{};
   a.c = attn_call(s, Q, K, V, O, kv_len, scale);
-  a.tiles = p.tiles, a.splits = p.splits, a.total = (int)p.total;
+  a.cut = p.cut;
   a.R = s.Nq * (s.H / s.Hkv);
+  a.rows = p.rows;
   a.heads = s.H;
   a.lse = lse;
-  const long rows = (long)s.B * s.Hkv * a.R;
+  const long parts = cut_left(p.cut) * p.cut.splits * p.rows;  // rows of partial sums
   a.part = (float*)ws;
-  a.ml = (float2*)((float*)ws + rows * p.splits * s.d);
-  const auto kernel = s.bf16 ? (p.qw == 1 ? attn_bf16_kernel<1> : attn_bf16_kernel<4>)
+  a.ml = (float2*)((float*)ws + parts * s.d);
+  const auto kernel = s.bf16 ? (p.rows == 32 ? attn_bf16_kernel<1> : attn_bf16_kernel<4>)
                              : (s.d == 64 ? attn_f32x_kernel<64> : attn_f32x_kernel<128>);
-  hipLaunchKernelGGL(kernel, dim3((unsigned)p.total), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)p.cut.total), dim3(256), 0, st, a);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.splits == 1) return e;
+  if (e != hipSuccess || parts == 0) return e;
   const auto join = s.bf16 ? attn_join_kernel<bf16, 128>
                            : s.d == 64 ? attn_join_kernel<float, 64> : attn_join_kernel<float, 128>;
-  hipLaunchKernelGGL(join, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a, rows);
+  hipLaunchKernelGGL(join, dim3((unsigned)(cut_left(p.cut) * p.rows / 4)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

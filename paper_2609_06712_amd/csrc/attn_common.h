@@ -51,6 +51,74 @@ __device__ __forceinline__ f32x4 mfma_f32(float a, float b, const f32x4& c) {
   return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 
+// How a pass over (b, key head, tile) is cut into workgroups. The first `whole` tiles, whole rounds of the
+// workgroups that the chip holds, have one each; the `left` ones of the last, partial round are given to `splits`
+// workgroups each, which take a part of the tile's walk and leave partial sums, so that the chip is full to the
+// end (8400 tokens, 12 heads: 792 tiles of dK/dV on 256 CUs are three rounds and 24 tiles). A causal pass has its
+// long walks first and short ones to fill the end with, so it is cut only where the tiles are fewer than
+// one round.
+struct Cut {
+  int tiles, bh, whole, splits, total, causal;
+};
+struct Part {
+  int tile, b, hk;
+  int split, splits;
+  int left;  // which of the cut tiles, -1 for a whole one
+  long bh;
+};
+// The tile at a place in the order. last_first: the last one has the longest walk (rows of a causal call).
+__device__ __forceinline__ void cut_tile(const Cut& c, int idx, bool last_first, int* tile, long* bh) {
+  const int t = c.causal ? idx / c.bh : idx % c.tiles;
+  *bh = c.causal ? idx % c.bh : idx / c.tiles;
+  *tile = c.causal && last_first ? c.tiles - 1 - t : t;
+}
+// And the place of a tile.
+__device__ __forceinline__ int cut_place(const Cut& c, int tile, long bh, bool last_first) {
+  if (!c.causal) return (int)(bh * c.tiles + tile);
+  return (last_first ? c.tiles - 1 - tile : tile) * c.bh + (int)bh;
+}
+__device__ __forceinline__ Part part_of(const Cut& c, int Hkv, int wg, bool last_first) {
+  Part p;
+  int idx;
+  if (wg < c.whole) {
+    idx = c.causal ? wg : xcd_remap(wg, c.whole);
+    p.split = 0, p.splits = 1, p.left = -1;
+  } else {
+    const int m = xcd_remap(wg - c.whole, c.total - c.whole);
+    p.left = m / c.splits;
+    p.split = m % c.splits, p.splits = c.splits;
+    idx = c.whole + p.left;
+  }
+  cut_tile(c, idx, last_first, &p.tile, &p.bh);
+  p.b = (int)(p.bh / Hkv);
+  p.hk = (int)(p.bh % Hkv);
+  return p;
+}
+// slots: workgroups that the chip holds; steps: of a whole walk; step_us: what one lasts; part_bytes: partial sums
+// of one part; least: steps that a part has at least.
+inline Cut make_cut(int tiles, int bh, bool causal, int slots, int steps, double step_us, double part_bytes,
+                    int least) {
+  Cut c{tiles, bh, 0, 1, 0, causal};
+  const long all = (long)tiles * bh;
+  long left = all % slots;
+  if (causal && all >= slots) left = 0;
+  if (left > 0) {
+    // rounds of a part's walk and its set-up (about two steps), then the sums written, read and one more launch
+    double best = -1;
+    for (int s = 1; s <= 64 && (s == 1 || (steps + s - 1) / s >= least); ++s) {
+      const double rounds = (double)((left * s + slots - 1) / slots);
+      double us = rounds * ((steps + s - 1) / s + 2) * step_us;
+      if (s > 1) us += 5 + 2 * left * s * part_bytes / 4e6;
+      if (best < 0 || us < 0.97 * best) best = us, c.splits = s;
+    }
+  }
+  if (c.splits == 1) left = 0;
+  c.whole = (int)(all - left);
+  c.total = (int)(c.whole + left * c.splits);
+  return c;
+}
+inline long cut_left(const Cut& c) { return c.splits > 1 ? (c.total - c.whole) / c.splits : 0; }
+
 // s_waitcnt vmcnt(N), the other counters free.
 template <int N>
 __device__ __forceinline__ void wait_vm() {

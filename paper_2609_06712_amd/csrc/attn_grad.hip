@@ -14,8 +14,8 @@
 // Row statistics: per query lse and D, in tiles of 32 queries [32 lse][32 D], per head padded to whole tiles with
 // lse = inf: P is then zero for rows past the last and for rows that see no key, with no test in the walk.
 //
-// When a pass has too few workgroups for the chip, each tile's walk is cut into parts whose fp32 sums go to the
-// workspace and are added in order by attn_sum_kernel.
+// The tiles that do not fill a round of the chip are cut (Cut); the parts' fp32 sums go to the workspace and are
+// added in order by attn_sum_kernel.
 #include <algorithm>
 
 #include "attn_common.h"
@@ -30,34 +30,38 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 struct GradArgs {
   AttnCall c;     // c.O: dO
   View G1, G2;    // dQ; or dK, dV
-  int tiles, splits, total, R, Np, H;
+  Cut cut;
+  int R, Np, H;
   const float* stat;   // [B, H, Np / 32][lse, D][32]
   const float* lse;    // [B, H, Nq], the forward's
-  float* part;         // splits > 1: [B Hkv][splits][rows][d], dV's after dK's
-  long part2;          // elements between dK's and dV's partials
+  float* dsum;         // attn_rowsum_bf16_kernel: D of the whole tiles' rows [B Hkv][R]
+  float* part;         // sums of the cut tiles: [left][splits][rows of a tile][d] (D: without d), dV's after dK's
+  long part2;          // elements between dK's and dV's
 };
 
 // Where the statistics of query i of a head are: lse there, D 32 further.
 __device__ __forceinline__ long stat_at(long head, int Np, int i) { return (head * (Np / 32) + i / 32) * 64 + i % 32; }
 
-// lse and D = the sum of `splits` parts [bh][split][R] (row i G + g of the key head bh) into tiles.
-__global__ __launch_bounds__(256) void attn_stat_kernel(int H, int G, int Nq, int Np, int splits, long rows,
-                                                        const float* __restrict__ lse,
-                                                        const float* __restrict__ part, float* __restrict__ stat) {
+// lse and D (of a cut tile the sum of its parts) into tiles; queries as rows i G + g of their key head.
+__global__ __launch_bounds__(256) void attn_stat_kernel(const GradArgs a, long rows, float* __restrict__ stat) {
   const long row = (long)blockIdx.x * 256 + threadIdx.x;  // (b, h, padded query)
   if (row >= rows) return;
-  const long bh = row / Np;
-  const int i = (int)(row % Np);
+  const int G = a.c.G, S = a.cut.splits;
+  const long head = row / a.Np, bh = head / G;
+  const int i = (int)(row % a.Np);
   float l = -__builtin_inff(), s = 0.f;
-  if (i < Nq) {
-    l = lse[bh * Nq + i];
-    const int h = (int)(bh % H);
-    const long R = (long)Nq * G;
-    const float* p = part + (bh / H * (H / G) + h / G) * splits * R + (long)i * G + h % G;
-    for (int k = 0; k < splits; ++k) s += p[k * R];
+  if (i < a.c.Nq) {
+    l = a.lse[head * a.c.Nq + i];
+    const int r = i * G + (int)(head % G), place = cut_place(a.cut, r / 256, bh, true);
+    if (place < a.cut.whole) {
+      s = a.dsum[bh * a.R + r];
+    } else {
+      const float* p = a.part + (long)(place - a.cut.whole) * S * 256 + r % 256;
+      for (int k = 0; k < S; ++k) s += p[k * 256];
+    }
   }
   const bool none = l == -__builtin_inff();
-  float* at = stat + stat_at(bh, Np, i);
+  float* at = stat + stat_at(head, a.Np, i);
   at[0] = none ? __builtin_inff() : l;
   at[32] = none ? 0.f : s;
 }
@@ -92,21 +96,6 @@ __global__ __launch_bounds__(256) void attn_rowdot_f32_kernel(int H, int Nq, int
 
 // ---- dQ ------------------------------------------------------------------------------------------------
 
-struct Part {
-  int tile, split, b, hk;
-  long bh;
-};
-__device__ __forceinline__ Part part_of(const GradArgs& a, int L, bool longest_last) {
-  Part p;
-  const int t = L % a.tiles, rest = L / a.tiles;
-  p.tile = longest_last ? a.tiles - 1 - t : t;
-  p.split = rest % a.splits;
-  p.bh = rest / a.splits;
-  p.b = (int)(p.bh / a.c.Hkv);
-  p.hk = (int)(p.bh % a.c.Hkv);
-  return p;
-}
-
 // Stores 128 channels of a row from the accumulator layout of a 32x32 tile set, rounded to bf16.
 __device__ __forceinline__ void store_row_bf16(char* row, const f32x16 (&acc)[4], float f, int hh) {
 #pragma unroll
@@ -127,14 +116,14 @@ __global__ __launch_bounds__(256, 2) void attn_rowsum_bf16_kernel(const GradArgs
   constexpr int STAGE = 2 * kTile, NBUF = 3, DPW = 2;
   __shared__ __attribute__((aligned(1024))) char lds[NBUF * STAGE];
   const AttnCall& c = a.c;
-  const Part pt = part_of(a, xcd_remap(blockIdx.x, a.total), c.causal);
+  const Part pt = part_of(a.cut, c.Hkv, blockIdx.x, true);
   const int wave = wave_uniform(threadIdx.x / 64), lane = threadIdx.x % 64, hh = lane / 32;
   const int n = attn_keys(c, pt.b);
   const int row0 = (pt.tile * 4 + wave) * 64;
   const int lim_lo = attn_limit(c, n, min(row0, a.R - 1) / c.G);
   const int lim_hi = row0 < a.R ? attn_limit(c, n, min(row0 + 63, a.R - 1) / c.G) : 0;
   const int end = max(0, attn_limit(c, n, min(pt.tile * 256 + 255, a.R - 1) / c.G));
-  const int all = (end + 31) / 32, per = (all + a.splits - 1) / a.splits;
+  const int all = (end + 31) / 32, per = (all + pt.splits - 1) / pt.splits;
   const int first = pt.split * per, T = max(0, min(all, first + per) - first);
   const char* Kh = c.K.p + pt.b * c.K.b + pt.hk * c.K.h;
   const char* Vh = c.V.p + pt.b * c.V.b + pt.hk * c.V.h;
@@ -237,7 +226,11 @@ __global__ __launch_bounds__(256, 2) void attn_rowsum_bf16_kernel(const GradArgs
   for (int u = 0; u < 2; ++u) {
     const int r = row0 + 32 * u + lane % 32;
     const float s = halves_sum(sum[u]);
-    if (r < a.R && hh == 0) a.part[(pt.bh * a.splits + pt.split) * a.R + r] = s;
+    if (r >= a.R || hh != 0) continue;
+    if (pt.left >= 0)
+      a.part[((long)pt.left * pt.splits + pt.split) * 256 + wave * 64 + 32 * u + lane] = s;
+    else
+      a.dsum[pt.bh * a.R + r] = s;
   }
 }
 
@@ -249,7 +242,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_bf16_kernel(const GradArgs a) 
   constexpr int STAGE = 2 * kTile, NBUF = 3, DPW = 2;
   __shared__ __attribute__((aligned(1024))) char lds[NBUF * STAGE];
   const AttnCall& c = a.c;
-  const Part pt = part_of(a, xcd_remap(blockIdx.x, a.total), c.causal);
+  const Part pt = part_of(a.cut, c.Hkv, blockIdx.x, true);
   const int wave = wave_uniform(threadIdx.x / 64), lane = threadIdx.x % 64, hh = lane / 32;
   const int n = attn_keys(c, pt.b);
   const int row0 = (pt.tile * 4 + wave) * 32;
@@ -258,7 +251,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_bf16_kernel(const GradArgs a) 
   const int lim_lo = attn_limit(c, n, min(row0, a.R - 1) / c.G);
   const int lim_hi = row0 < a.R ? attn_limit(c, n, min(row0 + 31, a.R - 1) / c.G) : 0;
   const int end = max(0, attn_limit(c, n, min(pt.tile * 128 + 127, a.R - 1) / c.G));
-  const int all = (end + 31) / 32, per = (all + a.splits - 1) / a.splits;
+  const int all = (end + 31) / 32, per = (all + pt.splits - 1) / pt.splits;
   const int first = pt.split * per, T = max(0, min(all, first + per) - first);
   const char* Kh = c.K.p + pt.b * c.K.b + pt.hk * c.K.h;
   const char* Vh = c.V.p + pt.b * c.V.b + pt.hk * c.V.h;
@@ -377,9 +370,9 @@ __global__ __launch_bounds__(256, 2) void attn_dq_bf16_kernel(const GradArgs a) 
     }
   }
   if (row0 + lane % 32 >= a.R) return;
-  if (a.splits > 1)
-    store_grad_row<false>(a.part + ((pt.bh * a.splits + pt.split) * a.R + r) * 128, acc, c.scale, hh, nullptr,
-                          nullptr);
+  if (pt.left >= 0)
+    store_grad_row<false>(a.part + (((long)pt.left * pt.splits + pt.split) * 128 + wave * 32 + lane % 32) * 128, acc,
+                          c.scale, hh, nullptr, nullptr);
   else
     store_row_bf16(a.G1.p + pt.b * a.G1.b + head * a.G1.h + i * a.G1.n, acc, c.scale, hh);
 }
@@ -390,7 +383,7 @@ __global__ __launch_bounds__(256) void attn_dq_f32_kernel(const GradArgs a) {
   constexpr int W = D / 16, LD = D + 4, PT = 32 * D / 4 / 256;
   __shared__ __attribute__((aligned(16))) float ks[32 * LD], vs[32 * LD];
   const AttnCall& c = a.c;
-  const Part pt = part_of(a, xcd_remap(blockIdx.x, a.total), c.causal);
+  const Part pt = part_of(a.cut, c.Hkv, blockIdx.x, true);
   const int wave = wave_uniform(threadIdx.x / 64), lane = threadIdx.x % 64, gr = lane / 16;
   const int n = attn_keys(c, pt.b);
   const int row0 = pt.tile * 64 + wave * 16;
@@ -398,7 +391,7 @@ __global__ __launch_bounds__(256) void attn_dq_f32_kernel(const GradArgs a) {
   const int lim = attn_limit(c, n, i);
   const int lim_hi = row0 < a.R ? attn_limit(c, n, min(row0 + 15, a.R - 1) / c.G) : 0;
   const int end = max(0, attn_limit(c, n, min(pt.tile * 64 + 63, a.R - 1) / c.G));
-  const int all = (end + 31) / 32, per = (all + a.splits - 1) / a.splits;
+  const int all = (end + 31) / 32, per = (all + pt.splits - 1) / pt.splits;
   const int t0 = pt.split * per, t1 = min(all, t0 + per);
   const char* Kh = c.K.p + pt.b * c.K.b + pt.hk * c.K.h;
   const char* Vh = c.V.p + pt.b * c.V.b + pt.hk * c.V.h;
@@ -447,8 +440,8 @@ __global__ __launch_bounds__(256) void attn_dq_f32_kernel(const GradArgs a) {
     }
   }
   if (row0 + lane % 16 >= a.R) return;
-  char* out = a.splits > 1
-                  ? reinterpret_cast<char*>(a.part + ((pt.bh * a.splits + pt.split) * a.R + r) * D)
+  char* out = pt.left >= 0
+                  ? reinterpret_cast<char*>(a.part + (((long)pt.left * pt.splits + pt.split) * 64 + wave * 16 + lane % 16) * D)
                   : a.G1.p + pt.b * a.G1.b + head * a.G1.h + i * a.G1.n;
   f32_store<D>(out, acc, c.scale, lane);
 }
@@ -460,13 +453,13 @@ __global__ __launch_bounds__(256) void attn_dq_f32_kernel(const GradArgs a) {
 struct Walk {
   int q0, tiles, t0, t1;  // first query (a multiple of 32), tiles per head, steps of this part
 };
-__device__ __forceinline__ Walk walk_of(const GradArgs& a, int n, int key0, int split) {
+__device__ __forceinline__ Walk walk_of(const GradArgs& a, int n, int key0, const Part& pt) {
   const AttnCall& c = a.c;
   Walk w;
   w.q0 = c.causal ? max(0, key0 - (n - c.Nq)) / 32 * 32 : 0;
   w.tiles = key0 < n && w.q0 < c.Nq ? (c.Nq - w.q0 + 31) / 32 : 0;
-  const int all = w.tiles * c.G, per = (all + a.splits - 1) / a.splits;
-  w.t0 = split * per;
+  const int all = w.tiles * c.G, per = (all + pt.splits - 1) / pt.splits;
+  w.t0 = pt.split * per;
   w.t1 = max(w.t0, min(all, w.t0 + per));
   return w;
 }
@@ -484,12 +477,12 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_bf16_kernel(const GradArgs a)
   constexpr int STAGE = 2 * kTile + 1024, DPW = 4, PBUF = 4 * 2048, NBUF = kDkvBuf;
   __shared__ __attribute__((aligned(1024))) char lds[NBUF * STAGE + 2 * PBUF];
   const AttnCall& c = a.c;
-  const Part pt = part_of(a, xcd_remap(blockIdx.x, a.total), false);
+  const Part pt = part_of(a.cut, c.Hkv, blockIdx.x, false);
   const int lane = threadIdx.x % 64, hh = lane / 32;
   const int wave = wave_uniform(threadIdx.x / 64), role = wave / 2, kw = wave % 2;
   const int n = attn_keys(c, pt.b), off = n - c.Nq;
   const int key0 = pt.tile * 128, key = key0 + kw * 64 + lane % 32;  // and key + 32
-  const Walk wk = walk_of(a, n, key0, pt.split);
+  const Walk wk = walk_of(a, n, key0, pt);
   const int T = wk.t1 - wk.t0;
 
   bf16x8 bf[2][8];
@@ -564,114 +557,97 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_bf16_kernel(const GradArgs a)
 #pragma unroll
       for (int s = 0; s < 8; ++s) fa[s] = row_frag(tile, lane % 32, s, hh);
     };
-    if (ROLE == 0) row_operands(lds);
     int buf = 0, back = NBUF - 1;  // stages of steps t and t - 1
-    for (int t = 0; t <= T; ++t) {
+    auto arrive = [&](int t) {
       if (issued >= t + 3)  // stage t + 1 has landed; one more step's loads may be under way
         wait_vm<DPW>();
       else
         wait_vm<0>();
       __syncthreads();
       if (issued < T) issue();
-      const int ahead = buf + 1 == NBUF ? 0 : buf + 1;
-      if (ROLE == 0 ? t < T : t > 0) {
-        const char* stage = lds + (ROLE ? back : buf) * STAGE;
-        char* pb = pbase + ((t - ROLE) & 1) * PBUF;
-        bf16x8 fb[8];
-        float4 lv[4];  // lse (role 0) or D (role 1) of the step's queries 8 j + 4 hh ..
-        f16x8 ph[2][2];
-        f32x16 X[2] = {f32x16{}, f32x16{}};
-        bf16x8 b2[2][2];
-        // P or dS of tile u
-        auto middle = [&](int u) {
-#pragma unroll
-          for (int k = 0; k < 16; ++k) {
-            const float v = k % 4 == 0 ? lv[k / 4].x : k % 4 == 1 ? lv[k / 4].y : k % 4 == 2 ? lv[k / 4].z : lv[k / 4].w;
-            if constexpr (ROLE == 0) {
-              const float p = __builtin_amdgcn_exp2f(fmaf(X[u][k], c.scale_log2, -v));
-              b2[u][k / 8][k % 8] = (bf16)p;
-              ph[u][k / 8][k % 8] = (_Float16)p;
-            } else {
-              b2[u][k / 8][k % 8] = (bf16)((float)ph[u][k / 8][k % 8] * (X[u][k] - v));
-            }
-          }
-          if constexpr (ROLE == 0) {
-            *reinterpret_cast<f16x8*>(pb + u * 2048) = ph[u][0];
-            *reinterpret_cast<f16x8*>(pb + u * 2048 + 1024) = ph[u][1];
-          }
-        };
-        auto hide = [&](int u) {  // P = 0 where the query is before the key
-          if (CAUSAL && ROLE == 0 && key0 + kw * 64 + 32 * u + 31 > cq + off) {
-            const int late = key + 32 * u - off - cq - 4 * hh;
-#pragma unroll
-            for (int k = 0; k < 16; ++k) X[u][k] = 8 * (k / 4) + k % 4 >= late ? X[u][k] : -__builtin_inff();
-          }
-        };
-#pragma unroll
-        for (int s = 0; s < 8; ++s) X[0] = mfma_bf16(fa[s], bf[0][s], X[0]);
-        if constexpr (ROLE == 1) {
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            ph[u][0] = *reinterpret_cast<const f16x8*>(pb + u * 2048);
-            ph[u][1] = *reinterpret_cast<const f16x8*>(pb + u * 2048 + 1024);
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          lv[j] = *reinterpret_cast<const float4*>(stage + 2 * kTile + ROLE * 128 + 32 * j + 16 * hh);
-#pragma unroll
-        for (int w = 0; w < 4; ++w)
-#pragma unroll
-          for (int v = 0; v < 2; ++v) fb[2 * w + v] = tr_frag(stage + (1 - ROLE) * kTile, w, v, lane);
-#pragma unroll
-        for (int s = 0; s < 8; ++s) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // MFMA
-          __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);  // DS reads
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        hide(0);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int s = 0; s < 8; ++s) X[1] = mfma_bf16(fa[s], bf[1][s], X[1]);
-        middle(0);
-#pragma unroll
-        for (int s = 0; s < 8; ++s) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x402, 8, 0);  // VALU, transcendentals
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        hide(1);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int v = 0; v < 2; ++v)
-#pragma unroll
-          for (int w = 0; w < 4; ++w) acc[0][w] = mfma_bf16(fb[2 * w + v], b2[0][v], acc[0][w]);
-        middle(1);
-#pragma unroll
-        for (int s = 0; s < 8; ++s) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x402, 8, 0);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        row_operands(lds + (ROLE ? buf : ahead) * STAGE + ROLE * kTile);
-#pragma unroll
-        for (int v = 0; v < 2; ++v)
-#pragma unroll
-          for (int w = 0; w < 4; ++w) acc[1][w] = mfma_bf16(fb[2 * w + v], b2[1][v], acc[1][w]);
-#pragma unroll
-        for (int s = 0; s < 8; ++s) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        cq += 32;
-        if (cq >= c.Nq) cq = wk.q0;
-      } else if (ROLE == 1 && t == 0) {
-        row_operands(lds + kTile);
-      }
+    };
+    auto advance = [&]() {
       back = buf;
-      buf = ahead;
+      buf = buf + 1 == NBUF ? 0 : buf + 1;
+    };
+    if (ROLE == 1) {
+      arrive(0);
+      advance();
     }
+    row_operands(lds + ROLE * kTile);
+    // (one straight body per role: with a test around it the accumulators move between register files)
+    for (int t = ROLE; t < T + ROLE; ++t) {
+      arrive(t);
+      const int ahead = buf + 1 == NBUF ? 0 : buf + 1;
+      const char* stage = lds + (ROLE ? back : buf) * STAGE;
+      char* pb = pbase + ((t - ROLE) & 1) * PBUF;
+      const char* tile = stage + (1 - ROLE) * kTile;                          // read transposed
+      const char* next = lds + (ROLE ? buf : ahead) * STAGE + ROLE * kTile;  // the next step's rows
+      bf16x8 fb[8];
+      float lv[16];  // lse (role 0) or D (role 1) of the step's queries 8 (k / 4) + 4 hh + k % 4
+      f16x8 ph[2][2];
+      f32x16 X[2] = {f32x16{}, f32x16{}};
+      bf16x8 b2[2][2];
+      // P or dS of two queries of tile u
+      auto middle = [&](int u, int k) {
+        if constexpr (ROLE == 0) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(X[u][k], c.scale_log2, -lv[k]));
+          const float q = __builtin_amdgcn_exp2f(fmaf(X[u][k + 1], c.scale_log2, -lv[k + 1]));
+          b2[u][k / 8][k % 8] = (bf16)p, b2[u][k / 8][k % 8 + 1] = (bf16)q;
+          ph[u][k / 8][k % 8] = (_Float16)p, ph[u][k / 8][k % 8 + 1] = (_Float16)q;
+          if (k % 8 == 6) *reinterpret_cast<f16x8*>(pb + u * 2048 + k / 8 * 1024) = ph[u][k / 8];
+        } else {
+          b2[u][k / 8][k % 8] = (bf16)((float)ph[u][k / 8][k % 8] * (X[u][k] - lv[k]));
+          b2[u][k / 8][k % 8 + 1] = (bf16)((float)ph[u][k / 8][k % 8 + 1] * (X[u][k + 1] - lv[k + 1]));
+        }
+      };
+      auto hide = [&](int u) {  // P = 0 where the query is before the key
+        if (CAUSAL && ROLE == 0 && key0 + kw * 64 + 32 * u + 31 > cq + off) {
+          const int late = key + 32 * u - off - cq - 4 * hh;
+#pragma unroll
+          for (int k = 0; k < 16; ++k) X[u][k] = 8 * (k / 4) + k % 4 >= late ? X[u][k] : -__builtin_inff();
+        }
+      };
+      // (the order between the barriers is the order of issue: a product, then what runs in its shadow)
+#pragma unroll
+      for (int s = 0; s < 8; ++s) {
+        X[0] = mfma_bf16(fa[s], bf[0][s], X[0]);
+        fb[s] = tr_frag(tile, s / 2, s % 2, lane);
+        if (s < 4) {
+          const float4 v = *reinterpret_cast<const float4*>(stage + 2 * kTile + ROLE * 128 + 32 * s + 16 * hh);
+          lv[4 * s] = v.x, lv[4 * s + 1] = v.y, lv[4 * s + 2] = v.z, lv[4 * s + 3] = v.w;
+        } else if (ROLE == 1) {
+          ph[s / 2 - 2][s % 2] = *reinterpret_cast<const f16x8*>(pb + (s / 2 - 2) * 2048 + s % 2 * 1024);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      hide(0);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int s = 0; s < 8; ++s) {
+        X[1] = mfma_bf16(fa[s], bf[1][s], X[1]);
+        middle(0, 2 * s);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      hide(1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int s = 0; s < 8; ++s) {
+        acc[0][s % 4] = mfma_bf16(fb[2 * (s % 4) + s / 4], b2[0][s / 4], acc[0][s % 4]);
+        middle(1, 2 * s);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int s = 0; s < 8; ++s) {
+        acc[1][s % 4] = mfma_bf16(fb[2 * (s % 4) + s / 4], b2[1][s / 4], acc[1][s % 4]);
+        fa[s] = row_frag(next, lane % 32, s, hh);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      cq += 32;
+      if (cq >= c.Nq) cq = wk.q0;
+      advance();
+    }
+    if (ROLE == 0) arrive(T);
   };
   if (T > 0) {
     if (role)
@@ -688,8 +664,8 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_bf16_kernel(const GradArgs a)
       for (int w = 0; w < 4; ++w) acc[u][w] = f32x16{};
     }
     const float f = role ? c.scale : 1.f;
-    if (a.splits > 1) {
-      float* out = a.part + (role ? 0 : a.part2) + ((pt.bh * a.splits + pt.split) * c.Nk + k) * 128;
+    if (pt.left >= 0) {
+      float* out = a.part + (role ? 0 : a.part2) + (((long)pt.left * pt.splits + pt.split) * 128 + k - key0) * 128;
       store_grad_row<false>(out, acc[u], f, hh, nullptr, nullptr);
     } else {
       const View& g = role ? a.G1 : a.G2;
@@ -705,11 +681,11 @@ __global__ __launch_bounds__(256) void attn_dkv_f32_kernel(const GradArgs a) {
   __shared__ __attribute__((aligned(16))) float qs[32 * LD], os[32 * LD];
   __shared__ float st[64];
   const AttnCall& c = a.c;
-  const Part pt = part_of(a, xcd_remap(blockIdx.x, a.total), false);
+  const Part pt = part_of(a.cut, c.Hkv, blockIdx.x, false);
   const int wave = wave_uniform(threadIdx.x / 64), lane = threadIdx.x % 64, gr = lane / 16;
   const int n = attn_keys(c, pt.b), off = n - c.Nq;
   const int key0 = pt.tile * 64, key = key0 + wave * 16 + lane % 16;
-  const Walk wk = walk_of(a, n, key0, pt.split);
+  const Walk wk = walk_of(a, n, key0, pt);
   float4 kv[W], vv[W];
   {
     const long k = max(0, min(key, n - 1));
@@ -773,8 +749,8 @@ __global__ __launch_bounds__(256) void attn_dkv_f32_kernel(const GradArgs a) {
   if (key >= c.Nk) return;
   const float live = key < n ? 1.f : 0.f;
   char *pk, *pv;
-  if (a.splits > 1) {
-    float* out = a.part + ((pt.bh * a.splits + pt.split) * c.Nk + key) * D;
+  if (pt.left >= 0) {
+    float* out = a.part + (((long)pt.left * pt.splits + pt.split) * 64 + key - key0) * D;
     pk = reinterpret_cast<char*>(out);
     pv = reinterpret_cast<char*>(out + a.part2);
   } else {
@@ -785,21 +761,23 @@ __global__ __launch_bounds__(256) void attn_dkv_f32_kernel(const GradArgs a) {
   f32_store<D>(pv, dv, live, lane);
 }
 
-// out row = sum of its parts, in order: part [B Hkv][splits][rows][D]; a row r is head hk G + r % G, token
-// r / G. A thread takes four channels.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void attn_sum_kernel(int Hkv, int G, int rows, int splits, long total,
+// The rows of the cut tiles: sum of their parts, in order. ROWS per tile; a row r is head hk G + r % G, token
+// r / G (G = 1: keys). A thread takes four channels.
+template <typename T, int D, int ROWS>
+__global__ __launch_bounds__(256) void attn_sum_kernel(const Cut cut, int Hkv, int G, int rows, bool last_first,
                                                        const float* __restrict__ part, View out) {
   const long e = (long)blockIdx.x * 256 + threadIdx.x;
-  const long at = e / (D / 4);
-  const int c = 4 * (int)(e % (D / 4));
-  if (at >= total) return;
-  const long bh = at / rows;
-  const int r = (int)(at % rows);
-  const float* src = part + (bh * splits * rows + r) * D + c;
+  const int c = 4 * (int)(e % (D / 4)), row = (int)(e / (D / 4) % ROWS);
+  const long left = e / (D / 4) / ROWS;
+  int tile;
+  long bh;
+  cut_tile(cut, cut.whole + (int)left, last_first, &tile, &bh);
+  const int r = tile * ROWS + row;
+  if (r >= rows) return;
+  const float* src = part + (left * cut.splits * ROWS + row) * D + c;
   float4 s = *reinterpret_cast<const float4*>(src);
-  for (int k = 1; k < splits; ++k) {
-    const float4 v = *reinterpret_cast<const float4*>(src + (long)k * rows * D);
+  for (int k = 1; k < cut.splits; ++k) {
+    const float4 v = *reinterpret_cast<const float4*>(src + (long)k * ROWS * D);
     s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
   }
   const int b = (int)(bh / Hkv), head = (int)(bh % Hkv) * G + r % G;
@@ -809,39 +787,39 @@ __global__ __launch_bounds__(256) void attn_sum_kernel(int Hkv, int G, int rows,
 
 struct GradPlan {
   int R, Np;
-  int qtiles, qsplits, ktiles, ksplits, dtiles, dsplits;
-  size_t stat, qpart, kpart, dpart;  // bytes, 256-aligned; kpart: of dK, and as many of dV
+  Cut d, q, k;                       // the passes of D (bf16), of dQ, of dK and dV
+  size_t stat, dsum, dpart, qpart, kpart;  // bytes, 256-aligned; kpart: of dK, and as many of dV
 };
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 GradPlan grad_plan(const AttnShape& s) {
-  GradPlan p;
-  const int G = s.H / s.Hkv;
-  const long bh = (long)s.B * s.Hkv;
+  GradPlan p{};
+  const int G = s.H / s.Hkv, bh = s.B * s.Hkv;
   p.R = s.Nq * G;
   p.Np = (s.Nq + 31) / 32 * 32;
-  const int qrows = s.bf16 ? 128 : 64, krows = s.bf16 ? 128 : 64;
-  p.qtiles = (p.R + qrows - 1) / qrows;
-  p.ktiles = (s.Nk + krows - 1) / krows;
-  // parts: one round of the workgroups that the chip holds, of at least 256 keys or 512 queries each
-  const long qhold = 2 * kCus, khold = (s.bf16 ? 1 : 2) * kCus;
-  p.qsplits = (int)std::max<long>(1, std::min<long>({qhold / (p.qtiles * bh), (s.Nk + 255) / 256, 64}));
-  p.ksplits = (int)std::max<long>(1, std::min<long>({khold / (p.ktiles * bh), ((long)p.R + 511) / 512, 64}));
-  p.dtiles = (p.R + 255) / 256;
-  p.dsplits = (int)std::max<long>(1, std::min<long>({qhold / (p.dtiles * bh), (s.Nk + 255) / 256, 64}));
+  const int rows = s.bf16 ? 128 : 64, keys = s.bf16 ? 128 : 64;
+  const int ksteps = (s.Nk + 31) / 32, qsteps = p.Np / 32 * G;
+  const double bytes = rows * s.d * 4.0;
+  p.q = make_cut((p.R + rows - 1) / rows, bh, s.causal, 2 * kCus, ksteps, s.bf16 ? 1.6 : 4.0, bytes, 8);
+  p.k = make_cut((s.Nk + keys - 1) / keys, bh, s.causal, (s.bf16 ? 1 : 2) * kCus, qsteps, s.bf16 ? 1.2 : 4.0,
+                 2 * bytes, 8);
   p.stat = up256((size_t)s.B * s.H * p.Np * 2 * sizeof(float));
-  p.dpart = s.bf16 ? up256((size_t)bh * p.dsplits * p.R * sizeof(float)) : 0;
-  p.qpart = p.qsplits > 1 ? up256((size_t)bh * p.qsplits * p.R * s.d * 4) : 0;
-  p.kpart = p.ksplits > 1 ? up256((size_t)bh * p.ksplits * s.Nk * s.d * 4) : 0;
+  if (s.bf16) {
+    p.d = make_cut((p.R + 255) / 256, bh, s.causal, 2 * kCus, ksteps, 1.3, 1024, 8);
+    p.dsum = up256((size_t)bh * p.R * sizeof(float));
+    p.dpart = up256((size_t)cut_left(p.d) * p.d.splits * 256 * sizeof(float));
+  }
+  p.qpart = up256((size_t)(cut_left(p.q) * p.q.splits * bytes));
+  p.kpart = up256((size_t)(cut_left(p.k) * p.k.splits * bytes));
   return p;
 }
 
-hipError_t launch_sum(const AttnShape& s, int G, int rows, int splits, const float* part, const View& out,
-                      hipStream_t st) {
-  const long total = (long)s.B * s.Hkv * rows, threads = total * (s.d / 4);
-  const auto k = s.bf16 ? attn_sum_kernel<bf16, 128>
-                        : s.d == 64 ? attn_sum_kernel<float, 64> : attn_sum_kernel<float, 128>;
-  hipLaunchKernelGGL(k, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, s.Hkv, G, rows, splits, total,
-                     part, out);
+hipError_t launch_sum(const AttnShape& s, const Cut& cut, int G, int rows, bool last_first, const float* part,
+                      const View& out, hipStream_t st) {
+  const int per = s.bf16 ? 128 : 64;
+  const unsigned grid = (unsigned)(cut_left(cut) * per * (s.d / 4) / 256);
+  const auto k = s.bf16 ? attn_sum_kernel<bf16, 128, 128>
+                        : s.d == 64 ? attn_sum_kernel<float, 64, 64> : attn_sum_kernel<float, 128, 64>;
+  hipLaunchKernelGGL(k, dim3(grid), dim3(256), 0, st, cut, s.Hkv, G, rows, last_first, part, out);
   return hipGetLastError();
 }
 
@@ -849,7 +827,7 @@ hipError_t launch_sum(const AttnShape& s, int G, int rows, int splits, const flo
 
 size_t attn_backward_workspace_bytes(const AttnShape& s) {
   const GradPlan p = grad_plan(s);
-  return p.stat + std::max({p.dpart, p.qpart, 2 * p.kpart});
+  return p.stat + std::max({p.dsum + p.dpart, p.qpart, 2 * p.kpart});
 }
 
 hipError_t launch_attn_backward(const AttnShape& s, const HeadView& Q, const HeadView& K, const HeadView& V,
@@ -863,44 +841,41 @@ hipError_t launch_attn_backward(const AttnShape& s, const HeadView& Q, const Hea
   float* stat = (float*)ws;
   a.stat = stat;
   a.lse = lse;
-  a.part = (float*)((char*)ws + p.stat);
+  float* rest = (float*)((char*)ws + p.stat);  // each pass's sums in turn
   const long rows = (long)s.B * s.H * p.Np;
   hipError_t e;
   if (s.bf16) {
-    a.tiles = p.dtiles, a.splits = p.dsplits, a.total = s.B * s.Hkv * p.dtiles * p.dsplits;
-    hipLaunchKernelGGL(attn_rowsum_bf16_kernel, dim3(a.total), dim3(256), 0, st, a);
+    a.cut = p.d;
+    a.dsum = rest;
+    a.part = (float*)((char*)rest + p.dsum);
+    hipLaunchKernelGGL(attn_rowsum_bf16_kernel, dim3(p.d.total), dim3(256), 0, st, a);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(attn_stat_kernel, dim3((unsigned)((rows + 255) / 256)), dim3(256), 0, st, s.H, s.H / s.Hkv,
-                       s.Nq, p.Np, p.dsplits, rows, lse, (const float*)a.part, stat);
+    hipLaunchKernelGGL(attn_stat_kernel, dim3((unsigned)((rows + 255) / 256)), dim3(256), 0, st, a, rows, stat);
   } else {
     hipLaunchKernelGGL(attn_rowdot_f32_kernel, dim3((unsigned)((rows * 16 + 255) / 256)), dim3(256), 0, st, s.H,
                        s.Nq, p.Np, s.d, rows, view_of(O, false), a.c.O, lse, stat);
   }
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const long bh = (long)s.B * s.Hkv;
+  a.part = rest;
   a.G1 = view_of(dQ, s.bf16);
-  a.tiles = p.qtiles, a.splits = p.qsplits, a.total = (int)(bh * p.qtiles * p.qsplits);
+  a.cut = p.q;
   const auto kq = s.bf16 ? attn_dq_bf16_kernel : s.d == 64 ? attn_dq_f32_kernel<64> : attn_dq_f32_kernel<128>;
-  hipLaunchKernelGGL(kq, dim3(a.total), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(kq, dim3(p.q.total), dim3(256), 0, st, a);
   e = hipGetLastError();
-  if (e == hipSuccess && p.qsplits > 1)
-    e = launch_sum(s, s.H / s.Hkv, p.R, p.qsplits, a.part, a.G1, st);
+  if (e == hipSuccess && p.qpart) e = launch_sum(s, p.q, s.H / s.Hkv, p.R, true, rest, a.G1, st);
   if (e != hipSuccess) return e;
   a.G1 = view_of(dK, s.bf16), a.G2 = view_of(dV, s.bf16);
-  a.tiles = p.ktiles, a.splits = p.ksplits, a.total = (int)(bh * p.ktiles * p.ksplits);
+  a.cut = p.k;
   a.part2 = (long)(p.kpart / sizeof(float));
-  if (s.bf16)
-    hipLaunchKernelGGL(s.causal ? attn_dkv_bf16_kernel<true> : attn_dkv_bf16_kernel<false>, dim3(a.total), dim3(256),
-                       0, st, a);
-  else
-    hipLaunchKernelGGL(s.d == 64 ? attn_dkv_f32_kernel<64> : attn_dkv_f32_kernel<128>, dim3(a.total), dim3(256),
-                       0, st, a);
+  const auto kk = s.bf16 ? (s.causal ? attn_dkv_bf16_kernel<true> : attn_dkv_bf16_kernel<false>)
+                         : s.d == 64 ? attn_dkv_f32_kernel<64> : attn_dkv_f32_kernel<128>;
+  hipLaunchKernelGGL(kk, dim3(p.k.total), dim3(256), 0, st, a);
   e = hipGetLastError();
-  if (e == hipSuccess && p.ksplits > 1) {
-    e = launch_sum(s, 1, s.Nk, p.ksplits, a.part, a.G1, st);
-    if (e == hipSuccess) e = launch_sum(s, 1, s.Nk, p.ksplits, a.part + a.part2, a.G2, st);
+  if (e == hipSuccess && p.kpart) {
+    e = launch_sum(s, p.k, 1, s.Nk, false, rest, a.G1, st);
+    if (e == hipSuccess) e = launch_sum(s, p.k, 1, s.Nk, false, rest + a.part2, a.G2, st);
   }
   return e;
 }
