@@ -16,7 +16,8 @@
 // The tiles of rows that do not fill a round of the chip are cut over their keys (Cut); the partial results (fp32,
 // with maximum and sum) are joined by attn_join_kernel in a fixed order.
 //
-// fp32 (d 64, 128), on fp32 matrix instructions (attn_common.h): workgroups of 64 rows, 16 per wave.
+// fp32 (d 64, 128), on fp32 matrix instructions (attn_common.h): workgroups of 64 rows, 16 per wave, or for few
+// rows of 16 with the keys dealt over the waves.
 #include <algorithm>
 
 #include "attn_common.h"
@@ -60,7 +61,7 @@ __global__ __launch_bounds__(256, QW == 4 ? 3 : 1) void attn_bf16_kernel(const F
   constexpr int STEP = QW == 4 ? 1 : 4;        // sub-tiles between two of a wave's
   __shared__ __attribute__((aligned(1024))) char lds[(QW == 4 ? 1 : 4) * NBUF * STAGE];
   const AttnCall& c = a.c;
-  const Part pt = part_of(a.cut, c.Hkv, blockIdx.x, true);
+  const Part pt = part_of(a.cut, c.Hkv, blockIdx.x);
   const int wave = wave_uniform(threadIdx.x / 64), lane = threadIdx.x % 64, hh = lane / 32;
   const int n = attn_keys(c, pt.b);
   const int row0 = (pt.tile * QW + (QW == 4 ? wave : 0)) * 32;  // first row of this wave
@@ -274,7 +275,7 @@ __global__ __launch_bounds__(256) void attn_f32x_kernel(const FwdArgs a) {
   constexpr int W = D / 16, LD = D + 4, PT = 32 * D / 4 / 256;  // 16-byte pieces per thread, tensor and tile
   __shared__ __attribute__((aligned(16))) float ks[32 * LD], vs[32 * LD];
   const AttnCall& c = a.c;
-  const Part pt = part_of(a.cut, c.Hkv, blockIdx.x, true);
+  const Part pt = part_of(a.cut, c.Hkv, blockIdx.x);
   const int wave = wave_uniform(threadIdx.x / 64), lane = threadIdx.x % 64, gr = lane / 16;
   const int n = attn_keys(c, pt.b);
   const int row0 = pt.tile * 64 + wave * 16;
@@ -353,6 +354,93 @@ __global__ __launch_bounds__(256) void attn_f32x_kernel(const FwdArgs a) {
     a.lse[(pt.b * a.heads + head) * c.Nq + i] = l > 0.f ? m + __log2f(l) : -__builtin_inff();
 }
 
+// fp32, few rows: a workgroup has 16 of them and its four waves take every fourth sub-tile of 16 keys, straight
+// from memory; they add up through LDS.
+template <int D>
+__global__ __launch_bounds__(256) void attn_f32_few_kernel(const FwdArgs a) {
+  constexpr int W = D / 16;
+  __shared__ __attribute__((aligned(16))) float os[4 * 16 * (D + 4)];
+  __shared__ float2 mls[4][16];
+  const AttnCall& c = a.c;
+  const Part pt = part_of(a.cut, c.Hkv, blockIdx.x);
+  const int wave = wave_uniform(threadIdx.x / 64), lane = threadIdx.x % 64, gr = lane / 16;
+  const int n = attn_keys(c, pt.b), row0 = pt.tile * 16;
+  const int r = min(row0 + lane % 16, a.R - 1), i = r / c.G, g = r % c.G;
+  const int lim = attn_limit(c, n, i);
+  const int end = max(0, attn_limit(c, n, min(row0 + 15, a.R - 1) / c.G));
+  const int all = (end + 15) / 16, per = (all + pt.splits - 1) / pt.splits;
+  const int t0 = pt.split * per, t1 = min(all, t0 + per);
+  const char* Kh = c.K.p + pt.b * c.K.b + pt.hk * c.K.h;
+  const char* Vh = c.V.p + pt.b * c.V.b + pt.hk * c.V.h;
+  float4 qv[W], kv[W], vv[4][D / 64];
+  f32_quarter<D>(c.Q.p + pt.b * c.Q.b + (pt.hk * c.G + g) * c.Q.h + i * c.Q.n, lane, qv);
+  f32x4 acc[W];
+#pragma unroll
+  for (int w = 0; w < W; ++w) acc[w] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = kNoMax, l = 0.f;
+  auto keys = [&](int t) { f32_quarter<D>(Kh + min(t * 16 + lane % 16, n - 1) * c.K.n, lane, kv); };
+  auto values = [&](int t) { f32_pieces<D>(Vh, c.V.n, t * 16, n - 1, lane, vv); };
+  if (t0 + wave < t1) {
+    keys(t0 + wave);
+    values(t0 + wave);
+  }
+  for (int t = t0 + wave; t < t1; t += 4) {
+    const int nxt = min(t + 4, t1 - 1);
+    const f32x4 sc = f32_rows<D>(kv, qv);
+    keys(nxt);
+    float p[4], mx = -__builtin_inff();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {  // key 16 t + 4 gr + k
+      p[k] = 16 * t + 4 * gr + k < lim ? sc[k] * c.scale_log2 : -__builtin_inff();
+      mx = fmaxf(mx, p[k]);
+    }
+    const float mnew = fmaxf(m, rows_max(mx)), alpha = __builtin_amdgcn_exp2f(m - mnew);
+    m = mnew;
+    l *= alpha;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      p[k] = __builtin_amdgcn_exp2f(p[k] - mnew);
+      l += p[k];
+    }
+#pragma unroll
+    for (int w = 0; w < W; ++w) acc[w] *= alpha;
+    f32_cols<D>(vv, p, acc);
+    values(nxt);
+  }
+  l = rows_sum(l);
+  if (gr == 0) mls[wave][lane] = make_float2(m, l);
+  __syncthreads();
+  float mx = kNoMax, sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) mx = fmaxf(mx, mls[w][lane % 16].x);
+  const float f = __builtin_amdgcn_exp2f(m - mx);
+#pragma unroll
+  for (int w = 0; w < W; ++w) acc[w] *= f;
+  float o[W];
+  f32_join<D>(os, acc, wave, lane, o);
+  const int row = threadIdx.x / 16, rr = row0 + row, c0 = (threadIdx.x % 16) * W;
+  if (rr >= a.R) return;
+  mx = kNoMax;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) mx = fmaxf(mx, mls[w][row].x);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) sum = fmaf(__builtin_amdgcn_exp2f(mls[w][row].x - mx), mls[w][row].y, sum);
+  const int ii = rr / c.G, head = pt.hk * c.G + rr % c.G;
+  const long at = ((long)pt.left * pt.splits + pt.split) * 16 + row;
+  const float inv = pt.left >= 0 ? 1.f : sum > 0.f ? 1.f / sum : 0.f;
+  float* out = pt.left >= 0 ? a.part + at * D
+                            : reinterpret_cast<float*>(c.O.p + pt.b * c.O.b + head * c.O.h + ii * c.O.n);
+#pragma unroll
+  for (int s = 0; s < W / 4; ++s)
+    reinterpret_cast<float4*>(out + c0)[s] =
+        make_float4(o[4 * s] * inv, o[4 * s + 1] * inv, o[4 * s + 2] * inv, o[4 * s + 3] * inv);
+  if (c0 != 0) return;
+  if (pt.left >= 0)
+    a.ml[at] = make_float2(mx, sum);
+  else if (a.lse)
+    a.lse[(pt.b * a.heads + head) * c.Nq + ii] = sum > 0.f ? mx + __log2f(sum) : -__builtin_inff();
+}
+
 // Joins the parts of a cut tile's rows: a wave per row, D / 64 channels per lane.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void attn_join_kernel(const FwdArgs a) {
@@ -364,26 +452,38 @@ __global__ __launch_bounds__(256) void attn_join_kernel(const FwdArgs a) {
   const int row = (int)(at % a.rows);
   int tile;
   long bh;
-  cut_tile(a.cut, a.cut.whole + (int)left, true, &tile, &bh);
+  cut_tile(a.cut, a.cut.whole + (int)left, &tile, &bh);
   const int r = tile * a.rows + row;
   if (r >= a.R) return;
-  const float2* ml = a.ml + left * S * a.rows + row;
+  // lane s: the weight of part s (at most 64); then the parts' rows, eight in flight
+  const float2 v = lane < S ? a.ml[(left * S + lane) * a.rows + row] : make_float2(kNoMax, 0.f);
   const float* part = a.part + (left * S * a.rows + row) * D + lane * V;
-  float mx = kNoMax;
-  for (int s = 0; s < S; ++s) mx = fmaxf(mx, ml[(long)s * a.rows].x);
-  float sum = 0.f, o[V] = {};
-  for (int s = 0; s < S; ++s) {
-    const float2 v = ml[(long)s * a.rows];
-    const float f = __builtin_amdgcn_exp2f(v.x - mx);
-    sum = fmaf(f, v.y, sum);
+  float mx = rows_max(v.x);
 #pragma unroll
-    for (int k = 0; k < V; ++k) o[k] = fmaf(f, part[(long)s * a.rows * D + k], o[k]);
+  for (int d = 8; d >= 1; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
+  const float f = __builtin_amdgcn_exp2f(v.x - mx);
+  float sum = rows_sum(f * v.y);
+#pragma unroll
+  for (int d = 8; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
+  float o[V] = {};
+  for (int s0 = 0; s0 < S; s0 += 8) {
+    float x[8][V];
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+#pragma unroll
+      for (int k = 0; k < V; ++k) x[u][k] = part[(long)min(s0 + u, S - 1) * a.rows * D + k];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const float w = s0 + u < S ? __shfl(f, s0 + u) : 0.f;
+#pragma unroll
+      for (int k = 0; k < V; ++k) o[k] = fmaf(w, x[u][k], o[k]);
+    }
   }
   const int b = (int)(bh / c.Hkv), i = r / c.G, head = (int)(bh % c.Hkv) * c.G + r % c.G;
-  const float f = sum > 0.f ? 1.f / sum : 0.f;
+  const float inv = sum > 0.f ? 1.f / sum : 0.f;
   T* out = reinterpret_cast<T*>(c.O.p + b * c.O.b + head * c.O.h + i * c.O.n) + lane * V;
 #pragma unroll
-  for (int k = 0; k < V; ++k) out[k] = from_f32<T>(o[k] * f);
+  for (int k = 0; k < V; ++k) out[k] = from_f32<T>(o[k] * inv);
   if (a.lse && lane == 0)
     a.lse[(b * a.heads + head) * c.Nq + i] = sum > 0.f ? mx + __log2f(sum) : -__builtin_inff();
 }
@@ -395,11 +495,13 @@ struct FwdPlan {
 };
 FwdPlan fwd_plan(const AttnShape& s) {
   const int R = s.Nq * (s.H / s.Hkv), bh = s.B * s.Hkv, steps = (s.Nk + 31) / 32;
-  const int rows = !s.bf16 ? 64 : R <= 32 ? 32 : 128, tiles = (R + rows - 1) / rows;
+  // few rows. bf16: bound by reading K and V, in parts of a quarter round, which also evens out samples of
+  // different lengths; fp32: by latency, when 64-row tiles leave CUs with less than two workgroups
+  const bool few = s.bf16 ? R <= 32 : f32_few((R + 63) / 64, bh);
+  const int rows = few ? (s.bf16 ? 32 : 16) : s.bf16 ? 128 : 64, tiles = (R + rows - 1) / rows;
   const double bytes = rows * (s.d + 2) * 4.0;
-  // few rows: bound by reading K and V, in parts of a quarter round, which also evens out samples of different
-  // lengths
-  if (s.bf16 && R <= 32) return {rows, make_cut(tiles, bh, false, 4 * kCus, steps, 0.4, bytes, 16)};
+  if (few && s.bf16) return {rows, make_cut(tiles, bh, false, 4 * kCus, steps, 0.4, bytes, 16)};
+  if (few) return {rows, make_cut(tiles, bh, s.causal, 4 * kCus, (s.Nk + 63) / 64, 1.5, bytes, 2)};
   return {rows, make_cut(tiles, bh, s.causal, s.bf16 ? 3 * kCus : 4 * kCus, steps, s.bf16 ? 0.9 : 2.0, bytes, 8)};
 }
 
@@ -424,8 +526,9 @@ hipError_t launch_attn(const AttnShape& s, const HeadView& Q, const HeadView& K,
   const long parts = cut_left(p.cut) * p.cut.splits * p.rows;  // rows of partial sums
   a.part = (float*)ws;
   a.ml = (float2*)((float*)ws + parts * s.d);
-  const auto kernel = s.bf16 ? (p.rows == 32 ? attn_bf16_kernel<1> : attn_bf16_kernel<4>)
-                             : (s.d == 64 ? attn_f32x_kernel<64> : attn_f32x_kernel<128>);
+  const auto kernel = s.bf16         ? (p.rows == 32 ? attn_bf16_kernel<1> : attn_bf16_kernel<4>)
+                      : p.rows == 16 ? (s.d == 64 ? attn_f32_few_kernel<64> : attn_f32_few_kernel<128>)
+                                     : (s.d == 64 ? attn_f32x_kernel<64> : attn_f32x_kernel<128>);
   hipLaunchKernelGGL(kernel, dim3((unsigned)p.cut.total), dim3(256), 0, st, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || parts == 0) return e;

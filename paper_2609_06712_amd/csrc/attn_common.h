@@ -54,9 +54,8 @@ __device__ __forceinline__ f32x4 mfma_f32(float a, float b, const f32x4& c) {
 // How a pass over (b, key head, tile) is cut into workgroups. The first `whole` tiles, whole rounds of the
 // workgroups that the chip holds, have one each; the `left` ones of the last, partial round are given to `splits`
 // workgroups each, which take a part of the tile's walk and leave partial sums, so that the chip is full to the
-// end (8400 tokens, 12 heads: 792 tiles of dK/dV on 256 CUs are three rounds and 24 tiles). A causal pass has its
-// long walks first and short ones to fill the end with, so it is cut only where the tiles are fewer than
-// one round.
+// end (8400 tokens, 12 heads: 792 tiles of dK/dV on 256 CUs are three rounds and 24 tiles). A causal pass has
+// walks of all lengths and no rounds, so it is cut only where the tiles are fewer than one round.
 struct Cut {
   int tiles, bh, whole, splits, total, causal;
 };
@@ -66,22 +65,24 @@ struct Part {
   int left;  // which of the cut tiles, -1 for a whole one
   long bh;
 };
-// The tile at a place in the order. last_first: the last one has the longest walk (rows of a causal call).
-__device__ __forceinline__ void cut_tile(const Cut& c, int idx, bool last_first, int* tile, long* bh) {
-  const int t = c.causal ? idx / c.bh : idx % c.tiles;
-  *bh = c.causal ? idx % c.bh : idx / c.tiles;
-  *tile = c.causal && last_first ? c.tiles - 1 - t : t;
+// The tile at a place in the order: heads one after the other, so that an XCD's share is whole heads; in a
+// causal call a head's long and short walks by turns, so that every share has as much work.
+__device__ __forceinline__ void cut_tile(const Cut& c, int idx, int* tile, long* bh) {
+  const int t = idx % c.tiles;
+  *bh = idx / c.tiles;
+  *tile = !c.causal ? t : t % 2 ? t / 2 : c.tiles - 1 - t / 2;
 }
 // And the place of a tile.
-__device__ __forceinline__ int cut_place(const Cut& c, int tile, long bh, bool last_first) {
-  if (!c.causal) return (int)(bh * c.tiles + tile);
-  return (last_first ? c.tiles - 1 - tile : tile) * c.bh + (int)bh;
+__device__ __forceinline__ int cut_place(const Cut& c, int tile, long bh) {
+  int t = tile;
+  if (c.causal) t = 2 * (c.tiles - 1 - tile) < c.tiles ? 2 * (c.tiles - 1 - tile) : 2 * tile + 1;
+  return (int)(bh * c.tiles + t);
 }
-__device__ __forceinline__ Part part_of(const Cut& c, int Hkv, int wg, bool last_first) {
+__device__ __forceinline__ Part part_of(const Cut& c, int Hkv, int wg) {
   Part p;
   int idx;
   if (wg < c.whole) {
-    idx = c.causal ? wg : xcd_remap(wg, c.whole);
+    idx = xcd_remap(wg, c.whole);
     p.split = 0, p.splits = 1, p.left = -1;
   } else {
     const int m = xcd_remap(wg - c.whole, c.total - c.whole);
@@ -89,7 +90,7 @@ __device__ __forceinline__ Part part_of(const Cut& c, int Hkv, int wg, bool last
     p.split = m % c.splits, p.splits = c.splits;
     idx = c.whole + p.left;
   }
-  cut_tile(c, idx, last_first, &p.tile, &p.bh);
+  cut_tile(c, idx, &p.tile, &p.bh);
   p.b = (int)(p.bh / Hkv);
   p.hk = (int)(p.bh % Hkv);
   return p;
@@ -117,6 +118,8 @@ inline Cut make_cut(int tiles, int bh, bool causal, int slots, int steps, double
   c.total = (int)(c.whole + left * c.splits);
   return c;
 }
+// fp32: tiles of 64 rows are so few that latency bounds them; 16-row tiles whose walk four waves share then.
+inline bool f32_few(long tiles, long bh) { return tiles * bh < 2 * kCus; }
 inline long cut_left(const Cut& c) { return c.splits > 1 ? (c.total - c.whole) / c.splits : 0; }
 
 // s_waitcnt vmcnt(N), the other counters free.
@@ -141,40 +144,65 @@ constexpr float kNoMax = -3e38f;
 
 // ---- fp32 tiles -------------------------------------------------------------------------------------
 // On v_mfma_f32_16x16x4_f32 (A: row l%16, k = l/16; B: column l%16, k = l/16; D: column l%16, rows
-// 4(l/16) + i) with 16-row tiles in LDS, rows padded to D + 4 floats:
+// 4(l/16) + i) with 16-row tiles:
 //   f32_rows   X Y^T, X the tile, Y a row per lane in registers; step s of lane group g contracts channel
 //              g D/4 + s, so that both sides are read as 16-byte pieces;
 //   f32_cols   acc += X^T p, p[i] the value of tile row 4g + i (where f32_rows leaves it); row l%16 of channel
 //              tile w is channel (l%16) D/16 + w, again whole pieces.
 template <int D>
-__device__ __forceinline__ f32x4 f32_rows(const float* tile, const float4 (&y)[D / 16], int lane) {
-  const float* row = tile + (lane % 16) * (D + 4) + (lane / 16) * (D / 4);
+__device__ __forceinline__ f32x4 f32_rows(const float4 (&x)[D / 16], const float4 (&y)[D / 16]) {
   f32x4 s0 = f32x4{0.f, 0.f, 0.f, 0.f}, s1 = s0;
 #pragma unroll
   for (int s = 0; s < D / 16; ++s) {
-    const float4 x = *reinterpret_cast<const float4*>(row + 4 * s);
-    s0 = mfma_f32(x.x, y[s].x, s0);
-    s1 = mfma_f32(x.y, y[s].y, s1);
-    s0 = mfma_f32(x.z, y[s].z, s0);
-    s1 = mfma_f32(x.w, y[s].w, s1);
+    s0 = mfma_f32(x[s].x, y[s].x, s0);
+    s1 = mfma_f32(x[s].y, y[s].y, s1);
+    s0 = mfma_f32(x[s].z, y[s].z, s0);
+    s1 = mfma_f32(x[s].w, y[s].w, s1);
   }
   return s0 + s1;
 }
 template <int D>
-__device__ __forceinline__ void f32_cols(const float* tile, const float (&p)[4], f32x4 (&acc)[D / 16],
-                                         int lane) {
-  constexpr int W = D / 16;
-  const float* at = tile + 4 * (lane / 16) * (D + 4) + (lane % 16) * W;
+__device__ __forceinline__ void f32_cols(const float4 (&x)[4][D / 64], const float (&p)[4], f32x4 (&acc)[D / 16]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int s = 0; s < W / 4; ++s) {
-      const float4 x = *reinterpret_cast<const float4*>(at + i * (D + 4) + 4 * s);
-      acc[4 * s] = mfma_f32(x.x, p[i], acc[4 * s]);
-      acc[4 * s + 1] = mfma_f32(x.y, p[i], acc[4 * s + 1]);
-      acc[4 * s + 2] = mfma_f32(x.z, p[i], acc[4 * s + 2]);
-      acc[4 * s + 3] = mfma_f32(x.w, p[i], acc[4 * s + 3]);
+    for (int s = 0; s < D / 64; ++s) {
+      acc[4 * s] = mfma_f32(x[i][s].x, p[i], acc[4 * s]);
+      acc[4 * s + 1] = mfma_f32(x[i][s].y, p[i], acc[4 * s + 1]);
+      acc[4 * s + 2] = mfma_f32(x[i][s].z, p[i], acc[4 * s + 2]);
+      acc[4 * s + 3] = mfma_f32(x[i][s].w, p[i], acc[4 * s + 3]);
     }
+}
+// The operands from a tile in LDS, rows padded to D + 4 floats.
+template <int D>
+__device__ __forceinline__ f32x4 f32_rows(const float* tile, const float4 (&y)[D / 16], int lane) {
+  const float* row = tile + (lane % 16) * (D + 4) + (lane / 16) * (D / 4);
+  float4 x[D / 16];
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) x[s] = *reinterpret_cast<const float4*>(row + 4 * s);
+  return f32_rows<D>(x, y);
+}
+template <int D>
+__device__ __forceinline__ void f32_cols(const float* tile, const float (&p)[4], f32x4 (&acc)[D / 16],
+                                         int lane) {
+  const float* at = tile + 4 * (lane / 16) * (D + 4) + (lane % 16) * (D / 16);
+  float4 x[4][D / 64];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int s = 0; s < D / 64; ++s) x[i][s] = *reinterpret_cast<const float4*>(at + i * (D + 4) + 4 * s);
+  f32_cols<D>(x, p, acc);
+}
+// The second operand from memory: a lane's pieces of rows row0 + 4 g + i, those past `last` re-read that one.
+template <int D>
+__device__ __forceinline__ void f32_pieces(const char* base, long stride, int row0, int last, int lane,
+                                           float4 (&x)[4][D / 64]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const char* row = base + min(row0 + 4 * (lane / 16) + i, last) * stride;
+#pragma unroll
+    for (int s = 0; s < D / 64; ++s) x[i][s] = reinterpret_cast<const float4*>(row)[(lane % 16) * (D / 64) + s];
+  }
 }
 // A lane's quarter of a row, for f32_rows.
 template <int D>
@@ -182,6 +210,27 @@ __device__ __forceinline__ void f32_quarter(const char* row, int lane, float4 (&
   const float4* at = reinterpret_cast<const float4*>(row) + (lane / 16) * (D / 16);
 #pragma unroll
   for (int s = 0; s < D / 16; ++s) y[s] = at[s];
+}
+// Adds up the accumulators of four waves for the same 16 rows, in order, through LDS [4][16][D + 4]: thread
+// tid has channels (tid % 16) W .. of row tid / 16.
+template <int D>
+__device__ __forceinline__ void f32_join(float* lds, const f32x4 (&acc)[D / 16], int wave, int lane,
+                                         float (&o)[D / 16]) {
+  constexpr int W = D / 16;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int s = 0; s < W / 4; ++s)
+      *reinterpret_cast<float4*>(lds + (wave * 16 + lane % 16) * (D + 4) + (4 * (lane / 16) + i) * W + 4 * s) =
+          make_float4(acc[4 * s][i], acc[4 * s + 1][i], acc[4 * s + 2][i], acc[4 * s + 3][i]);
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < W; ++k) {
+    o[k] = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) o[k] += lds[(w * 16 + threadIdx.x / 16) * (D + 4) + (threadIdx.x % 16) * W + k];
+  }
 }
 // Stores a row from f32_cols' accumulators (lane: row l%16, channels (4g + i) W + w), scaled by f.
 template <int D>

@@ -52,7 +52,7 @@ __global__ __launch_bounds__(256) void attn_stat_kernel(const GradArgs a, long r
   float l = -__builtin_inff(), s = 0.f;
   if (i < a.c.Nq) {
     l = a.lse[head * a.c.Nq + i];
-    const int r = i * G + (int)(head % G), place = cut_place(a.cut, r / 256, bh, true);
+    const int r = i * G + (int)(head % G), place = cut_place(a.cut, r / 256, bh);
     if (place < a.cut.whole) {
       s = a.dsum[bh * a.R + r];
     } else {
@@ -116,7 +116,7 @@ __global__ __launch_bounds__(256, 2) void attn_rowsum_bf16_kernel(const GradArgs
   constexpr int STAGE = 2 * kTile, NBUF = 3, DPW = 2;
   __shared__ __attribute__((aligned(1024))) char lds[NBUF * STAGE];
   const AttnCall& c = a.c;
-  const Part pt = part_of(a.cut, c.Hkv, blockIdx.x, true);
+  const Part pt = part_of(a.cut, c.Hkv, blockIdx.x);
   const int wave = wave_uniform(threadIdx.x / 64), lane = threadIdx.x % 64, hh = lane / 32;
   const int n = attn_keys(c, pt.b);
   const int row0 = (pt.tile * 4 + wave) * 64;
@@ -242,7 +242,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_bf16_kernel(const GradArgs a) 
   constexpr int STAGE = 2 * kTile, NBUF = 3, DPW = 2;
   __shared__ __attribute__((aligned(1024))) char lds[NBUF * STAGE];
   const AttnCall& c = a.c;
-  const Part pt = part_of(a.cut, c.Hkv, blockIdx.x, true);
+  const Part pt = part_of(a.cut, c.Hkv, blockIdx.x);
   const int wave = wave_uniform(threadIdx.x / 64), lane = threadIdx.x % 64, hh = lane / 32;
   const int n = attn_keys(c, pt.b);
   const int row0 = (pt.tile * 4 + wave) * 32;
@@ -383,7 +383,7 @@ __global__ __launch_bounds__(256) void attn_dq_f32_kernel(const GradArgs a) {
   constexpr int W = D / 16, LD = D + 4, PT = 32 * D / 4 / 256;
   __shared__ __attribute__((aligned(16))) float ks[32 * LD], vs[32 * LD];
   const AttnCall& c = a.c;
-  const Part pt = part_of(a.cut, c.Hkv, blockIdx.x, true);
+  const Part pt = part_of(a.cut, c.Hkv, blockIdx.x);
   const int wave = wave_uniform(threadIdx.x / 64), lane = threadIdx.x % 64, gr = lane / 16;
   const int n = attn_keys(c, pt.b);
   const int row0 = pt.tile * 64 + wave * 16;
@@ -446,6 +446,58 @@ __global__ __launch_bounds__(256) void attn_dq_f32_kernel(const GradArgs a) {
   f32_store<D>(out, acc, c.scale, lane);
 }
 
+// fp32, few rows: 16 per workgroup, every fourth sub-tile of 16 keys per wave, straight from memory.
+template <int D>
+__global__ __launch_bounds__(256) void attn_dq_f32_few_kernel(const GradArgs a) {
+  constexpr int W = D / 16;
+  __shared__ __attribute__((aligned(16))) float os[4 * 16 * (D + 4)];
+  const AttnCall& c = a.c;
+  const Part pt = part_of(a.cut, c.Hkv, blockIdx.x);
+  const int wave = wave_uniform(threadIdx.x / 64), lane = threadIdx.x % 64, gr = lane / 16;
+  const int n = attn_keys(c, pt.b), row0 = pt.tile * 16;
+  const int r = min(row0 + lane % 16, a.R - 1), i = r / c.G, head = pt.hk * c.G + r % c.G;
+  const int lim = attn_limit(c, n, i);
+  const int end = max(0, attn_limit(c, n, min(row0 + 15, a.R - 1) / c.G));
+  const int all = (end + 15) / 16, per = (all + pt.splits - 1) / pt.splits;
+  const int t0 = pt.split * per, t1 = min(all, t0 + per);
+  const char* Kh = c.K.p + pt.b * c.K.b + pt.hk * c.K.h;
+  const char* Vh = c.V.p + pt.b * c.V.b + pt.hk * c.V.h;
+  float4 qv[W], dv[W];
+  f32_quarter<D>(c.Q.p + pt.b * c.Q.b + head * c.Q.h + i * c.Q.n, lane, qv);
+  f32_quarter<D>(c.O.p + pt.b * c.O.b + head * c.O.h + i * c.O.n, lane, dv);
+  const float* st = a.stat + stat_at((long)pt.b * a.H + head, a.Np, i);
+  const float lse = st[0], dsum = st[32];
+  f32x4 acc[W];
+#pragma unroll
+  for (int w = 0; w < W; ++w) acc[w] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int t = t0 + wave; t < t1; t += 4) {
+    float4 kv[W], vv[W], kc[4][D / 64];
+    const long key = min(t * 16 + lane % 16, n - 1);
+    f32_quarter<D>(Kh + key * c.K.n, lane, kv);
+    f32_quarter<D>(Vh + key * c.V.n, lane, vv);
+    f32_pieces<D>(Kh, c.K.n, t * 16, n - 1, lane, kc);
+    const f32x4 sc = f32_rows<D>(kv, qv), dp = f32_rows<D>(vv, dv);
+    float ds[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float p = 16 * t + 4 * gr + k < lim ? __builtin_amdgcn_exp2f(fmaf(sc[k], c.scale_log2, -lse)) : 0.f;
+      ds[k] = p * (dp[k] - dsum);
+    }
+    f32_cols<D>(kc, ds, acc);
+  }
+  float o[W];
+  f32_join<D>(os, acc, wave, lane, o);
+  const int row = threadIdx.x / 16, rr = row0 + row;
+  if (rr >= a.R) return;
+  float* out = pt.left >= 0
+                   ? a.part + (((long)pt.left * pt.splits + pt.split) * 16 + row) * D
+                   : reinterpret_cast<float*>(a.G1.p + pt.b * a.G1.b + (pt.hk * c.G + rr % c.G) * a.G1.h + (rr / c.G) * a.G1.n);
+#pragma unroll
+  for (int s = 0; s < W / 4; ++s)
+    reinterpret_cast<float4*>(out + (threadIdx.x % 16) * W)[s] =
+        make_float4(o[4 * s] * c.scale, o[4 * s + 1] * c.scale, o[4 * s + 2] * c.scale, o[4 * s + 3] * c.scale);
+}
+
 // ---- dK, dV ----------------------------------------------------------------------------------------------
 
 // The walk of a block of keys: steps of 32 queries, the query heads of its key head one after the other, each from
@@ -477,7 +529,7 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_bf16_kernel(const GradArgs a)
   constexpr int STAGE = 2 * kTile + 1024, DPW = 4, PBUF = 4 * 2048, NBUF = kDkvBuf;
   __shared__ __attribute__((aligned(1024))) char lds[NBUF * STAGE + 2 * PBUF];
   const AttnCall& c = a.c;
-  const Part pt = part_of(a.cut, c.Hkv, blockIdx.x, false);
+  const Part pt = part_of(a.cut, c.Hkv, blockIdx.x);
   const int lane = threadIdx.x % 64, hh = lane / 32;
   const int wave = wave_uniform(threadIdx.x / 64), role = wave / 2, kw = wave % 2;
   const int n = attn_keys(c, pt.b), off = n - c.Nq;
@@ -681,7 +733,7 @@ __global__ __launch_bounds__(256) void attn_dkv_f32_kernel(const GradArgs a) {
   __shared__ __attribute__((aligned(16))) float qs[32 * LD], os[32 * LD];
   __shared__ float st[64];
   const AttnCall& c = a.c;
-  const Part pt = part_of(a.cut, c.Hkv, blockIdx.x, false);
+  const Part pt = part_of(a.cut, c.Hkv, blockIdx.x);
   const int wave = wave_uniform(threadIdx.x / 64), lane = threadIdx.x % 64, gr = lane / 16;
   const int n = attn_keys(c, pt.b), off = n - c.Nq;
   const int key0 = pt.tile * 64, key = key0 + wave * 16 + lane % 16;
@@ -761,17 +813,85 @@ __global__ __launch_bounds__(256) void attn_dkv_f32_kernel(const GradArgs a) {
   f32_store<D>(pv, dv, live, lane);
 }
 
+// fp32, few keys: 16 per workgroup, every fourth sub-tile of 16 queries per wave, straight from memory.
+template <int D>
+__global__ __launch_bounds__(256) void attn_dkv_f32_few_kernel(const GradArgs a) {
+  constexpr int W = D / 16;
+  __shared__ __attribute__((aligned(16))) float os[4 * 16 * (D + 4)];
+  const AttnCall& c = a.c;
+  const Part pt = part_of(a.cut, c.Hkv, blockIdx.x);
+  const int wave = wave_uniform(threadIdx.x / 64), lane = threadIdx.x % 64, gr = lane / 16;
+  const int n = attn_keys(c, pt.b), off = n - c.Nq;
+  const int key0 = pt.tile * 16, key = key0 + lane % 16;
+  const Walk wk = walk_of(a, n, key0, pt);
+  float4 kv[W], vv[W];
+  {
+    const long k = max(0, min(key, n - 1));
+    f32_quarter<D>(c.K.p + pt.b * c.K.b + pt.hk * c.K.h + k * c.K.n, lane, kv);
+    f32_quarter<D>(c.V.p + pt.b * c.V.b + pt.hk * c.V.h + k * c.V.n, lane, vv);
+  }
+  f32x4 dk[W], dv[W];
+#pragma unroll
+  for (int w = 0; w < W; ++w) dk[w] = dv[w] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int t = 2 * wk.t0 + wave; t < 2 * wk.t1; t += 4) {  // half steps
+    const int head = pt.hk * c.G + t / 2 / wk.tiles, q = wk.q0 + t / 2 % wk.tiles * 32 + t % 2 * 16;
+    if (q >= c.Nq) continue;
+    const char* Qh = c.Q.p + pt.b * c.Q.b + head * c.Q.h;
+    const char* Oh = c.O.p + pt.b * c.O.b + head * c.O.h;
+    const long i = min(q + lane % 16, c.Nq - 1);
+    float4 qv[W], ov[W], qc[4][D / 64], oc[4][D / 64];
+    f32_quarter<D>(Qh + i * c.Q.n, lane, qv);
+    f32_quarter<D>(Oh + i * c.O.n, lane, ov);
+    f32_pieces<D>(Qh, c.Q.n, q, c.Nq - 1, lane, qc);
+    f32_pieces<D>(Oh, c.O.n, q, c.Nq - 1, lane, oc);
+    const float* st = a.stat + stat_at((long)pt.b * a.H + head, a.Np, q + 4 * gr);
+    const float4 l4 = *reinterpret_cast<const float4*>(st), d4 = *reinterpret_cast<const float4*>(st + 32);
+    const f32x4 sc = f32_rows<D>(qv, kv), dp = f32_rows<D>(ov, vv);
+    const float lse[4] = {l4.x, l4.y, l4.z, l4.w}, dsum[4] = {d4.x, d4.y, d4.z, d4.w};
+    float p[4], ds[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {  // query q + 4 gr + k
+      const bool seen = !c.causal || key <= q + 4 * gr + k + off;
+      p[k] = seen ? __builtin_amdgcn_exp2f(fmaf(sc[k], c.scale_log2, -lse[k])) : 0.f;
+      ds[k] = p[k] * (dp[k] - dsum[k]);
+    }
+    f32_cols<D>(oc, p, dv);
+    f32_cols<D>(qc, ds, dk);
+  }
+  float ok[W], ov[W];
+  f32_join<D>(os, dk, wave, lane, ok);
+  f32_join<D>(os, dv, wave, lane, ov);
+  const int k = key0 + threadIdx.x / 16, c0 = (threadIdx.x % 16) * W;
+  if (k >= c.Nk) return;
+  const float live = k < n ? 1.f : 0.f, f = c.scale * live;
+  float *pk, *pv;
+  if (pt.left >= 0) {
+    pk = a.part + (((long)pt.left * pt.splits + pt.split) * 16 + k - key0) * D;
+    pv = pk + a.part2;
+  } else {
+    pk = reinterpret_cast<float*>(a.G1.p + pt.b * a.G1.b + pt.hk * a.G1.h + k * a.G1.n);
+    pv = reinterpret_cast<float*>(a.G2.p + pt.b * a.G2.b + pt.hk * a.G2.h + k * a.G2.n);
+  }
+#pragma unroll
+  for (int s = 0; s < W / 4; ++s) {
+    reinterpret_cast<float4*>(pk + c0)[s] =
+        make_float4(ok[4 * s] * f, ok[4 * s + 1] * f, ok[4 * s + 2] * f, ok[4 * s + 3] * f);
+    reinterpret_cast<float4*>(pv + c0)[s] =
+        make_float4(ov[4 * s] * live, ov[4 * s + 1] * live, ov[4 * s + 2] * live, ov[4 * s + 3] * live);
+  }
+}
+
 // The rows of the cut tiles: sum of their parts, in order. ROWS per tile; a row r is head hk G + r % G, token
 // r / G (G = 1: keys). A thread takes four channels.
 template <typename T, int D, int ROWS>
-__global__ __launch_bounds__(256) void attn_sum_kernel(const Cut cut, int Hkv, int G, int rows, bool last_first,
+__global__ __launch_bounds__(256) void attn_sum_kernel(const Cut cut, int Hkv, int G, int rows,
                                                        const float* __restrict__ part, View out) {
   const long e = (long)blockIdx.x * 256 + threadIdx.x;
   const int c = 4 * (int)(e % (D / 4)), row = (int)(e / (D / 4) % ROWS);
   const long left = e / (D / 4) / ROWS;
   int tile;
   long bh;
-  cut_tile(cut, cut.whole + (int)left, last_first, &tile, &bh);
+  cut_tile(cut, cut.whole + (int)left, &tile, &bh);
   const int r = tile * ROWS + row;
   if (r >= rows) return;
   const float* src = part + (left * cut.splits * ROWS + row) * D + c;
@@ -786,8 +906,8 @@ __global__ __launch_bounds__(256) void attn_sum_kernel(const Cut cut, int Hkv, i
 }
 
 struct GradPlan {
-  int R, Np;
-  Cut d, q, k;                       // the passes of D (bf16), of dQ, of dK and dV
+  int R, Np, rows, keys;  // rows and keys of a tile
+  Cut d, q, k;            // the passes of D (bf16), of dQ, of dK and dV
   size_t stat, dsum, dpart, qpart, kpart;  // bytes, 256-aligned; kpart: of dK, and as many of dV
 };
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -796,30 +916,39 @@ GradPlan grad_plan(const AttnShape& s) {
   const int G = s.H / s.Hkv, bh = s.B * s.Hkv;
   p.R = s.Nq * G;
   p.Np = (s.Nq + 31) / 32 * 32;
-  const int rows = s.bf16 ? 128 : 64, keys = s.bf16 ? 128 : 64;
   const int ksteps = (s.Nk + 31) / 32, qsteps = p.Np / 32 * G;
-  const double bytes = rows * s.d * 4.0;
-  p.q = make_cut((p.R + rows - 1) / rows, bh, s.causal, 2 * kCus, ksteps, s.bf16 ? 1.6 : 4.0, bytes, 8);
-  p.k = make_cut((s.Nk + keys - 1) / keys, bh, s.causal, (s.bf16 ? 1 : 2) * kCus, qsteps, s.bf16 ? 1.2 : 4.0,
-                 2 * bytes, 8);
+  if (s.bf16) {
+    p.rows = p.keys = 128;
+  } else {
+    p.rows = f32_few((p.R + 63) / 64, bh) ? 16 : 64;
+    p.keys = f32_few((s.Nk + 63) / 64, bh) ? 16 : 64;
+  }
+  const int qtiles = (p.R + p.rows - 1) / p.rows, ktiles = (s.Nk + p.keys - 1) / p.keys;
+  const double qbytes = p.rows * s.d * 4.0, kbytes = p.keys * s.d * 4.0;
+  p.q = s.bf16          ? make_cut(qtiles, bh, s.causal, 2 * kCus, ksteps, 1.6, qbytes, 8)
+        : p.rows == 64 ? make_cut(qtiles, bh, s.causal, 2 * kCus, ksteps, 3.0, qbytes, 4)
+                       : make_cut(qtiles, bh, s.causal, 2 * kCus, (ksteps + 1) / 2, 2.5, qbytes, 2);
+  p.k = s.bf16          ? make_cut(ktiles, bh, s.causal, kCus, qsteps, 1.2, 2 * kbytes, 8)
+        : p.keys == 64 ? make_cut(ktiles, bh, s.causal, 2 * kCus, qsteps, 4.0, 2 * kbytes, 4)
+                       : make_cut(ktiles, bh, s.causal, 2 * kCus, (qsteps + 1) / 2, 3.5, 2 * kbytes, 2);
   p.stat = up256((size_t)s.B * s.H * p.Np * 2 * sizeof(float));
   if (s.bf16) {
     p.d = make_cut((p.R + 255) / 256, bh, s.causal, 2 * kCus, ksteps, 1.3, 1024, 8);
     p.dsum = up256((size_t)bh * p.R * sizeof(float));
     p.dpart = up256((size_t)cut_left(p.d) * p.d.splits * 256 * sizeof(float));
   }
-  p.qpart = up256((size_t)(cut_left(p.q) * p.q.splits * bytes));
-  p.kpart = up256((size_t)(cut_left(p.k) * p.k.splits * bytes));
+  p.qpart = up256((size_t)(cut_left(p.q) * p.q.splits * qbytes));
+  p.kpart = up256((size_t)(cut_left(p.k) * p.k.splits * kbytes));
   return p;
 }
 
-hipError_t launch_sum(const AttnShape& s, const Cut& cut, int G, int rows, bool last_first, const float* part,
+hipError_t launch_sum(const AttnShape& s, const Cut& cut, int per, int G, int rows, const float* part,
                       const View& out, hipStream_t st) {
-  const int per = s.bf16 ? 128 : 64;
-  const unsigned grid = (unsigned)(cut_left(cut) * per * (s.d / 4) / 256);
-  const auto k = s.bf16 ? attn_sum_kernel<bf16, 128, 128>
-                        : s.d == 64 ? attn_sum_kernel<float, 64, 64> : attn_sum_kernel<float, 128, 64>;
-  hipLaunchKernelGGL(k, dim3(grid), dim3(256), 0, st, cut, s.Hkv, G, rows, last_first, part, out);
+  const long threads = cut_left(cut) * per * (s.d / 4);  // a multiple of 256: per is one of 16
+  const auto k = s.bf16      ? attn_sum_kernel<bf16, 128, 128>
+                 : per == 16 ? (s.d == 64 ? attn_sum_kernel<float, 64, 16> : attn_sum_kernel<float, 128, 16>)
+                             : (s.d == 64 ? attn_sum_kernel<float, 64, 64> : attn_sum_kernel<float, 128, 64>);
+  hipLaunchKernelGGL(k, dim3((unsigned)(threads / 256)), dim3(256), 0, st, cut, s.Hkv, G, rows, part, out);
   return hipGetLastError();
 }
 
@@ -861,21 +990,24 @@ hipError_t launch_attn_backward(const AttnShape& s, const HeadView& Q, const Hea
   a.part = rest;
   a.G1 = view_of(dQ, s.bf16);
   a.cut = p.q;
-  const auto kq = s.bf16 ? attn_dq_bf16_kernel : s.d == 64 ? attn_dq_f32_kernel<64> : attn_dq_f32_kernel<128>;
+  const auto kq = s.bf16         ? attn_dq_bf16_kernel
+                  : p.rows == 16 ? (s.d == 64 ? attn_dq_f32_few_kernel<64> : attn_dq_f32_few_kernel<128>)
+                                 : (s.d == 64 ? attn_dq_f32_kernel<64> : attn_dq_f32_kernel<128>);
   hipLaunchKernelGGL(kq, dim3(p.q.total), dim3(256), 0, st, a);
   e = hipGetLastError();
-  if (e == hipSuccess && p.qpart) e = launch_sum(s, p.q, s.H / s.Hkv, p.R, true, rest, a.G1, st);
+  if (e == hipSuccess && p.qpart) e = launch_sum(s, p.q, p.rows, s.H / s.Hkv, p.R, rest, a.G1, st);
   if (e != hipSuccess) return e;
   a.G1 = view_of(dK, s.bf16), a.G2 = view_of(dV, s.bf16);
   a.cut = p.k;
   a.part2 = (long)(p.kpart / sizeof(float));
-  const auto kk = s.bf16 ? (s.causal ? attn_dkv_bf16_kernel<true> : attn_dkv_bf16_kernel<false>)
-                         : s.d == 64 ? attn_dkv_f32_kernel<64> : attn_dkv_f32_kernel<128>;
+  const auto kk = s.bf16         ? (s.causal ? attn_dkv_bf16_kernel<true> : attn_dkv_bf16_kernel<false>)
+                  : p.keys == 16 ? (s.d == 64 ? attn_dkv_f32_few_kernel<64> : attn_dkv_f32_few_kernel<128>)
+                                 : (s.d == 64 ? attn_dkv_f32_kernel<64> : attn_dkv_f32_kernel<128>);
   hipLaunchKernelGGL(kk, dim3(p.k.total), dim3(256), 0, st, a);
   e = hipGetLastError();
   if (e == hipSuccess && p.kpart) {
-    e = launch_sum(s, p.k, 1, s.Nk, false, rest, a.G1, st);
-    if (e == hipSuccess) e = launch_sum(s, p.k, 1, s.Nk, false, rest + a.part2, a.G2, st);
+    e = launch_sum(s, p.k, p.keys, 1, s.Nk, rest, a.G1, st);
+    if (e == hipSuccess) e = launch_sum(s, p.k, p.keys, 1, s.Nk, rest + a.part2, a.G2, st);
   }
   return e;
 }
