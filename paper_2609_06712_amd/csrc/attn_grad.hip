@@ -882,10 +882,13 @@ __global__ __launch_bounds__(256) void attn_dkv_f32_few_kernel(const GradArgs a)
 }
 
 // The rows of the cut tiles: sum of their parts, in order. ROWS per tile; a row r is head hk G + r % G, token
-// r / G (G = 1: keys). A thread takes four channels.
+// r / G (G = 1: keys). A thread takes four channels. gridDim.y = 2: a second set `part2` further, into out2.
 template <typename T, int D, int ROWS>
 __global__ __launch_bounds__(256) void attn_sum_kernel(const Cut cut, int Hkv, int G, int rows,
-                                                       const float* __restrict__ part, View out) {
+                                                       const float* __restrict__ part, long part2, View out1,
+                                                       View out2) {
+  const View out = blockIdx.y ? out2 : out1;
+  part += blockIdx.y * part2;
   const long e = (long)blockIdx.x * 256 + threadIdx.x;
   const int c = 4 * (int)(e % (D / 4)), row = (int)(e / (D / 4) % ROWS);
   const long left = e / (D / 4) / ROWS;
@@ -895,14 +898,19 @@ __global__ __launch_bounds__(256) void attn_sum_kernel(const Cut cut, int Hkv, i
   const int r = tile * ROWS + row;
   if (r >= rows) return;
   const float* src = part + (left * cut.splits * ROWS + row) * D + c;
-  float4 s = *reinterpret_cast<const float4*>(src);
-  for (int k = 1; k < cut.splits; ++k) {
-    const float4 v = *reinterpret_cast<const float4*>(src + (long)k * ROWS * D);
-    s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+  f32x4 s = *reinterpret_cast<const f32x4*>(src);
+  for (int k0 = 1; k0 < cut.splits; k0 += 8) {  // eight loads in flight
+    f32x4 v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      v[u] = *reinterpret_cast<const f32x4*>(src + (long)min(k0 + u, cut.splits - 1) * ROWS * D);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) s = k0 + u < cut.splits ? s + v[u] : s;
   }
   const int b = (int)(bh / Hkv), head = (int)(bh % Hkv) * G + r % G;
   T* o = reinterpret_cast<T*>(out.p + b * out.b + head * out.h + (long)(r / G) * out.n) + c;
-  o[0] = from_f32<T>(s.x), o[1] = from_f32<T>(s.y), o[2] = from_f32<T>(s.z), o[3] = from_f32<T>(s.w);
+  #pragma unroll
+  for (int k = 0; k < 4; ++k) o[k] = from_f32<T>(s[k]);
 }
 
 struct GradPlan {
@@ -942,13 +950,14 @@ GradPlan grad_plan(const AttnShape& s) {
   return p;
 }
 
-hipError_t launch_sum(const AttnShape& s, const Cut& cut, int per, int G, int rows, const float* part,
-                      const View& out, hipStream_t st) {
+hipError_t launch_sum(const AttnShape& s, const Cut& cut, int per, int G, int rows, int outs, const GradArgs& a,
+                      hipStream_t st) {
   const long threads = cut_left(cut) * per * (s.d / 4);  // a multiple of 256: per is one of 16
   const auto k = s.bf16      ? attn_sum_kernel<bf16, 128, 128>
                  : per == 16 ? (s.d == 64 ? attn_sum_kernel<float, 64, 16> : attn_sum_kernel<float, 128, 16>)
                              : (s.d == 64 ? attn_sum_kernel<float, 64, 64> : attn_sum_kernel<float, 128, 64>);
-  hipLaunchKernelGGL(k, dim3((unsigned)(threads / 256)), dim3(256), 0, st, cut, s.Hkv, G, rows, part, out);
+  hipLaunchKernelGGL(k, dim3((unsigned)(threads / 256), outs), dim3(256), 0, st, cut, s.Hkv, G, rows,
+                     (const float*)a.part, a.part2, a.G1, a.G2);
   return hipGetLastError();
 }
 
@@ -995,7 +1004,7 @@ hipError_t launch_attn_backward(const AttnShape& s, const HeadView& Q, const Hea
                                  : (s.d == 64 ? attn_dq_f32_kernel<64> : attn_dq_f32_kernel<128>);
   hipLaunchKernelGGL(kq, dim3(p.q.total), dim3(256), 0, st, a);
   e = hipGetLastError();
-  if (e == hipSuccess && p.qpart) e = launch_sum(s, p.q, p.rows, s.H / s.Hkv, p.R, rest, a.G1, st);
+  if (e == hipSuccess && p.qpart) e = launch_sum(s, p.q, p.rows, s.H / s.Hkv, p.R, 1, a, st);
   if (e != hipSuccess) return e;
   a.G1 = view_of(dK, s.bf16), a.G2 = view_of(dV, s.bf16);
   a.cut = p.k;
@@ -1005,10 +1014,7 @@ hipError_t launch_attn_backward(const AttnShape& s, const HeadView& Q, const Hea
                                  : (s.d == 64 ? attn_dkv_f32_kernel<64> : attn_dkv_f32_kernel<128>);
   hipLaunchKernelGGL(kk, dim3(p.k.total), dim3(256), 0, st, a);
   e = hipGetLastError();
-  if (e == hipSuccess && p.kpart) {
-    e = launch_sum(s, p.k, p.keys, 1, s.Nk, rest, a.G1, st);
-    if (e == hipSuccess) e = launch_sum(s, p.k, p.keys, 1, s.Nk, rest + a.part2, a.G2, st);
-  }
+  if (e == hipSuccess && p.kpart) e = launch_sum(s, p.k, p.keys, 1, s.Nk, 2, a, st);
   return e;
 }
 

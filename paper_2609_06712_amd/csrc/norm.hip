@@ -18,11 +18,17 @@ namespace {
 
 constexpr int kNormMax = 16384;
 
+// Sum over the wave, in every lane: the four 16-lane rows by permlane swaps, within a row by DPP (no LDS).
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float x) {
+  return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 15, 15, false));
+}
 __device__ __forceinline__ float wave_sum(float x) {
-  x = rows_sum(x);  // lanes l, l^16, l^32, l^48
-#pragma unroll
-  for (int off = 8; off >= 1; off >>= 1) x += __shfl_xor(x, off);
-  return x;
+  x = rows_sum(x);        // lanes l, l^16, l^32, l^48
+  x = dpp_add<0xB1>(x);   // l ^ 1
+  x = dpp_add<0x4E>(x);   // l ^ 2
+  x = dpp_add<0x141>(x);  // mirror of 8 lanes
+  return dpp_add<0x140>(x);  // mirror of 16
 }
 
 // Eight consecutive elements as loaded.
@@ -189,7 +195,7 @@ __global__ __launch_bounds__(norm_threads<TPR>()) void norm_fwd_kernel(const Nor
 
 // The backward of a chunk of rows: dx, and the chunk's sums of dy xh and dy into its partial.
 template <typename T, int TPR, int P>
-__global__ __launch_bounds__(norm_threads<TPR>()) void norm_bwd_kernel(const NormArgs a) {
+__global__ __launch_bounds__(norm_threads<TPR>(), sizeof(T) == 2 ? (P == 3 ? 3 : P == 4 ? 2 : 4) : (P == 1 ? 4 : 2)) void norm_bwd_kernel(const NormArgs a) {
   constexpr int THREADS = norm_threads<TPR>(), RPB = THREADS / TPR, WPR = TPR / 64;
   __shared__ float2 meet[2][WPR];
   __shared__ float sums[RPB > 1 ? THREADS : 1][8];
@@ -227,29 +233,31 @@ __global__ __launch_bounds__(norm_threads<TPR>()) void norm_bwd_kernel(const Nor
   int turn = 0;
   for (long rr = r0; rr < r1; rr += RPB, turn ^= 1) {
     const long r = rr + slot;
-    float xh[P][8], g[P][8], c1 = 0.f, c2 = 0.f;
+    Raw8<T> cx[P], cy[P];  // the row as loaded: taken apart twice, it leaves registers for a third wave per SIMD
+    float c1 = 0.f, c2 = 0.f;
     const float mu = nmu, rs = nrs;
 #pragma unroll
     for (int p = 0; p < P; ++p)
-      if (col[p] < d) {
-        unpack(nx[p], xh[p]);
-        unpack(ny[p], g[p]);
-      }
+      if (col[p] < d) cx[p] = nx[p], cy[p] = ny[p];
     fetch(r + RPB);
 #pragma unroll
     for (int p = 0; p < P; ++p)
-      if (col[p] < d)
+      if (col[p] < d) {
+        float xh[8], g[8];
+        unpack(cx[p], xh);
+        unpack(cy[p], g);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-          xh[p][k] = (xh[p][k] - mu) * rs;
+          xh[k] = (xh[k] - mu) * rs;
           if (RPB == 1 || r < r1) {
-            sw[p][k] = fmaf(g[p][k], xh[p][k], sw[p][k]);
-            sb[p][k] += g[p][k];
+            sw[p][k] = fmaf(g[k], xh[k], sw[p][k]);
+            sb[p][k] += g[k];
           }
-          g[p][k] *= w[p][k];
-          c1 += g[p][k];
-          c2 = fmaf(g[p][k], xh[p][k], c2);
+          g[k] *= w[p][k];
+          c1 += g[k];
+          c2 = fmaf(g[k], xh[k], c2);
         }
+      }
     c1 = wave_sum(c1);
     c2 = wave_sum(c2);
     if constexpr (WPR > 1) {
@@ -269,9 +277,11 @@ __global__ __launch_bounds__(norm_threads<TPR>()) void norm_bwd_kernel(const Nor
 #pragma unroll
       for (int p = 0; p < P; ++p)
         if (col[p] < d) {
-          float o[8];
+          float x[8], g[8], o[8];
+          unpack(cx[p], x);
+          unpack(cy[p], g);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) o[k] = rs * (g[p][k] - c1 - xh[p][k] * c2);
+          for (int k = 0; k < 8; ++k) o[k] = rs * (fmaf(g[k], w[p][k], -c1) - (x[k] - mu) * rs * c2);
           store8(DX + r * a.ldo + col[p], o);
         }
     }
@@ -298,11 +308,14 @@ __global__ __launch_bounds__(norm_threads<TPR>()) void norm_bwd_kernel(const Nor
     }
 }
 
-// Threads per row: a wave up to 2048 channels, where a row costs it no meeting with others; a workgroup
-// beyond, and for few rows, whose chain of loads and sums is then a quarter as long.
-int norm_row_threads(long rows, int d) {
+// Threads per row. Up to 2048 channels a wave, which has no meeting with others per row (forward, 65520 rows of
+// 1536: 85 us, 100 with 256 threads; backward 147 and 156); for few rows 256, whose chain of loads and sums is a
+// quarter as long. Beyond, 256 or 512: forward 75600 x 5120 314 us with 256, 390 with 512, backward 499
+// and 487; 8192 x 8192 backward 103 and 100.
+int norm_row_threads(long rows, int d, bool bwd) {
   if (d > 8192) return 512;
-  return d > 2048 || rows < kCus ? 256 : 64;
+  if (d > 2048) return bwd ? 512 : 256;
+  return rows < kCus ? 256 : 64;
 }
 
 template <typename T, bool BWD, int TPR>
@@ -338,21 +351,22 @@ hipError_t launch_norm_t(bool bf, const NormArgs& a, int tpr, dim3 grid, hipStre
   return hipGetLastError();
 }
 
-// Workgroups per group of rows: `want` over all groups, each of at least one turn of rows.
+// Workgroups per group of rows, each of at least one turn of rows. The forward takes many short ones (16 per CU of
+// 256 threads a row: 4096 channels 108 us, with 8 115; 512 threads: 16384 channels 56 with 4, 67 with 16), the
+// backward two per CU, as each leaves a partial of 2 d sums (65520 x 1536: 147 us, with 4 155, with 16 207).
 struct NormPlan {
   int tpr;
   long chunk;
   int chunks;
 };
-NormPlan norm_plan(const NormShape& s, long want) {
+NormPlan norm_plan(const NormShape& s, bool bwd) {
   const long per = s.rows / s.groups;
-  const int tpr = norm_row_threads(s.rows, s.d), side = tpr < 256 ? 256 / tpr : 1;
-  long n = (want + s.groups - 1) / s.groups;
-  long chunk = (per + n - 1) / n;
-  chunk = (chunk + side - 1) / side * side;
+  const int tpr = norm_row_threads(s.rows, s.d, bwd), side = tpr < 256 ? 256 / tpr : 1;
+  const long want = (bwd ? 2 : tpr == 64 ? 8 : tpr == 256 ? 16 : 4) * kCus;
+  const long n = (want + s.groups - 1) / s.groups;
+  const long chunk = ((per + n - 1) / n + side - 1) / side * side;
   return {tpr, chunk, (int)((per + chunk - 1) / chunk)};
 }
-constexpr long kNormFwdWgs = 8 * kCus, kNormBwdWgs = 4 * kCus;
 
 }  // namespace
 
@@ -360,7 +374,7 @@ int norm_max_channels() { return kNormMax; }
 
 hipError_t launch_norm(const NormShape& s, const void* X, long ldx, const void* W, const void* Bias,
                        float eps, void* Y, long ldy, float* mean, float* rstd, hipStream_t st) {
-  const NormPlan pl = norm_plan(s, kNormFwdWgs);
+  const NormPlan pl = norm_plan(s, false);
   NormArgs a{};
   a.per = s.rows / s.groups, a.chunk = pl.chunk, a.d = s.d, a.rms = s.rms, a.whalf = s.wbf16;
   a.ldx = ldx, a.ldo = ldy, a.eps = eps;
@@ -369,13 +383,13 @@ hipError_t launch_norm(const NormShape& s, const void* X, long ldx, const void* 
 }
 
 size_t norm_backward_workspace_bytes(const NormShape& s) {
-  return (size_t)norm_plan(s, kNormBwdWgs).chunks * s.groups * 2 * s.d * sizeof(float);
+  return (size_t)norm_plan(s, true).chunks * s.groups * 2 * s.d * sizeof(float);
 }
 
 hipError_t launch_norm_backward(const NormShape& s, const void* X, long ldx, const void* W,
                                 const float* mean, const float* rstd, const void* dY, long ldy, void* dX,
                                 long lddx, float* dW, float* dB, void* ws, hipStream_t st) {
-  const NormPlan pl = norm_plan(s, kNormBwdWgs);
+  const NormPlan pl = norm_plan(s, true);
   NormArgs a{};
   a.per = s.rows / s.groups, a.chunk = pl.chunk, a.d = s.d, a.rms = s.rms, a.whalf = s.wbf16;
   a.ldx = ldx, a.ldy = ldy, a.ldo = lddx;

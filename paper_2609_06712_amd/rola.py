@@ -893,11 +893,19 @@ def rola_gate_logits_backward(X, Wg, dlogits, grid, H=1, d_h=128, want_dX=True, 
 NORM_KIND = {"layer": 0, "rms": 1}
 
 
-def _on_current_device(x):
-    """The kernels run on the current device's stream."""
-    if x.get_device() != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on {x.device}, the current device is "
-                         f"cuda:{torch.cuda.current_device()}")
+# The current device without torch.cuda.current_device()'s checks (1 us a call); as _raw_stream, not part of
+# torch's public interface.
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _stream_here(x, stream):
+    """The stream of a call whose tensors must be on the current device: the kernels run there."""
+    device = x.get_device()
+    if device != _current_device():
+        raise ValueError(f"the tensors are on {x.device}, the current device is cuda:{_current_device()}")
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(device)
+    return _stream(stream)
 
 
 def _norm_rows(a, x, name, like=None):
@@ -930,8 +938,6 @@ def _norm_rows(a, x, name, like=None):
 
 def _norm_params(a, x, w, name, dtype=None):
     """Groups of rows that a weight [d], or [B, d] for x [B, N, d], gives."""
-    if w is None:
-        return None
     if not isinstance(w, torch.Tensor):
         raise ValueError(f"{name} must be a tensor")
     if dtype is None and w.dtype != torch.float32 and w.dtype != x.dtype:
@@ -967,7 +973,7 @@ def rola_norm(X, W=None, Bias=None, kind="layer", eps=1e-6, out=None, want_stats
         raise ValueError(f"kind must be one of {sorted(NORM_KIND)}, got {kind!r}")
     a = _Args()
     ldx = _norm_rows(a, X, "X")
-    groups = _norm_params(a, X, W, "W")
+    groups = None if W is None else _norm_params(a, X, W, "W")
     if Bias is not None:
         gb = _norm_params(a, X, Bias, "Bias", None if W is None else W.dtype)
         if groups is not None and gb != groups:
@@ -978,14 +984,14 @@ def rola_norm(X, W=None, Bias=None, kind="layer", eps=1e-6, out=None, want_stats
     else:
         ldy = _norm_rows(a, out, "out", X)
     a.done()
-    _on_current_device(X)
+    st = _stream_here(X, stream)
     mean = rstd = None
     if want_stats:
         rstd = torch.empty(X.shape[:-1], dtype=torch.float32, device=X.device)
         mean = torch.empty_like(rstd) if kind == "layer" else None
     prob = _norm_problem(*_norm_key(X, Bias if W is None else W, groups, kind))
     _check(LIB.rola_norm(prob, _ptr(X), ldx, _ptr(W), _ptr(Bias), eps, _ptr(out), ldy, _ptr(mean), _ptr(rstd),
-                         _stream(stream)), "rola_norm")
+                         st), "rola_norm")
     return out, mean, rstd
 
 
@@ -1004,7 +1010,7 @@ def rola_norm_backward(X, W, mean, rstd, dY, kind="layer", want_bias=True, per_s
     a = _Args()
     ldx = _norm_rows(a, X, "X")
     ldy = _norm_rows(a, dY, "dY", X)
-    groups = _norm_params(a, X, W, "W")
+    groups = None if W is None else _norm_params(a, X, W, "W")
     if groups is None:
         groups = X.shape[0] if per_sample and X.dim() == 3 else 1
     elif per_sample is not None and bool(per_sample) != (W.dim() == 2):
@@ -1021,7 +1027,7 @@ def rola_norm_backward(X, W, mean, rstd, dY, kind="layer", want_bias=True, per_s
         ws = torch.empty(max(_norm_ws(*key), 16), dtype=torch.uint8, device=X.device)
     a.workspace(ws)
     a.done()
-    _on_current_device(X)
+    st = _stream_here(X, stream)
     d = X.shape[-1]
     shape = (2, d) if groups == 1 else (2, groups, d)
     both = torch.empty(shape, dtype=torch.float32, device=X.device)
@@ -1030,7 +1036,7 @@ def rola_norm_backward(X, W, mean, rstd, dY, kind="layer", want_bias=True, per_s
     dW, dB = both[0], both[1] if want_bias else None
     _check(LIB.rola_norm_backward(_norm_problem(*key), _ptr(X), ldx, _ptr(W),
                                   _ptr(mean) if kind == "layer" else None, _ptr(rstd), _ptr(dY), ldy, _ptr(out),
-                                  ldo, _ptr(dW), _ptr(dB), _ptr(ws), ws.numel(), _stream(stream)),
+                                  ldo, _ptr(dW), _ptr(dB), _ptr(ws), ws.numel(), st),
            "rola_norm_backward")
     return out, dW, dB
 
@@ -1114,10 +1120,10 @@ def rola_attn(Q, K, V, kv_len=None, causal=False, scale=None, out=None, lse=None
         ws = torch.empty(need, dtype=torch.uint8, device=Q.device)
     a.workspace(ws)
     a.done()
-    _on_current_device(Q)
+    st = _stream_here(Q, stream)
     _check(LIB.rola_attn(_attn_problem(*key), hq, hk, hv, _ptr(kv_len),
                          key[5] ** -0.5 if scale is None else scale, ho, _ptr(lse), _ptr(ws),
-                         0 if ws is None else ws.numel(), _stream(stream)), "rola_attn")
+                         0 if ws is None else ws.numel(), st), "rola_attn")
     return out, lse
 
 
@@ -1140,8 +1146,8 @@ def rola_attn_backward(Q, K, V, O, lse, dO, kv_len=None, causal=False, scale=Non
         ws = torch.empty(_attn_ws(True, *key), dtype=torch.uint8, device=Q.device)
     a.workspace(ws)
     a.done()
-    _on_current_device(Q)
+    st = _stream_here(Q, stream)
     _check(LIB.rola_attn_backward(_attn_problem(*key), hq, hk, hv, _ptr(kv_len),
                                   key[5] ** -0.5 if scale is None else scale, ho, _ptr(lse), hg, gq, gk, gv,
-                                  _ptr(ws), ws.numel(), _stream(stream)), "rola_attn_backward")
+                                  _ptr(ws), ws.numel(), st), "rola_attn_backward")
     return dQ, dK, dV
