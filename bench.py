@@ -377,7 +377,8 @@ def train_bench(reps: int) -> None:
 
 def dit_bench(reps: int) -> None:
     """Per-block time of a synthetic Wan-shaped DiT block (random weights) with the RoLA module or
-    the dense attention kernel as its self-attention, and the implied DiT time per denoising step
+    the dense attention kernel as its self-attention, both also with this library's norms and
+    text cross-attention around it ("+ kernels around"), and the implied DiT time per denoising step
     (blocks x block time, one forward, no CFG). Printed as markdown."""
     from paper_2609_06712_amd import dit_block as DB
     print("## Synthetic Wan-shaped DiT block (random weights), bf16\n")
@@ -387,14 +388,15 @@ def dit_bench(reps: int) -> None:
     for shape in (DB.WAN_1_3B_480P, DB.WAN_14B_720P):
         x, ctx = DB.inputs(shape)
         res = {}
-        for attn in ("dense", "rola"):
-            blk = DB.DiTBlock(shape, attn=attn)
+        for attn, around in (("dense", "torch"), ("rola", "torch"), ("dense", "rola"), ("rola", "rola")):
+            blk = DB.DiTBlock(shape, attn=attn, around=around)
             h = torch.randn_like(x)
             sa = time_call(lambda: blk.self_attention(h), max(2, reps // 2 if attn == "dense" else reps))[0]
             bm = time_call(lambda: blk.forward(x, ctx), max(2, reps // 2 if attn == "dense" else reps))[0]
-            res[attn] = bm
-            ratio = f"{res['dense'] / bm:.2f}" if attn == "rola" else "-"
-            print(f"| {shape.name} | {'x'.join(map(str, shape.grid))} | {attn} | {sa:.2f} | {bm:.2f} | "
+            res[attn, around] = bm
+            ratio = f"{res['dense', around] / bm:.2f}" if attn == "rola" else "-"
+            label = attn + (" + kernels around" if around == "rola" else "")
+            print(f"| {shape.name} | {'x'.join(map(str, shape.grid))} | {label} | {sa:.2f} | {bm:.2f} | "
                   f"{shape.layers} | {bm * shape.layers:.0f} | {ratio} |", flush=True)
             del blk, h
             torch.cuda.empty_cache()

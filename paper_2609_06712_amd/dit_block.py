@@ -6,9 +6,10 @@ RMSNorm on q and k, output projection, cross-attention to text tokens, GELU MLP)
 self-attention is either the RoLA module (gate logits, backbone RoPE, block selection, low-rank
 summary, sparse attention with the low-rank readout and gated combine in its epilogue -- all this
 library's kernels) or this library's dense attention kernel. The projections and the MLP are plain
-library GEMMs (torch.matmul); the cross-attention is a plain chunked softmax attention (torch). The
-shapes follow the public Wan2.1 configurations; the weights are random, so only timing and plumbing
-are meaningful.
+library GEMMs (torch.matmul). The norms and the text cross-attention are plain torch by default, or with
+around="rola" this library's norms and its attention over another set of tokens, which takes q, k
+and v as views of the projections. The shapes follow the public Wan2.1 configurations; the weights are
+random, so only timing and plumbing are meaningful.
 """
 
 from __future__ import annotations
@@ -48,11 +49,15 @@ def _ln(x, eps=1e-6):
 
 
 class DiTBlock:
-    """One block; `attn` is "rola" or "dense". Weights are drawn from a seeded generator."""
+    """One block; `attn` is "rola" or "dense", `around` (the norms and the cross-attention) "torch" or
+    "rola". Weights are drawn from a seeded generator."""
 
     def __init__(self, shape: DiTShape, attn="rola", block=64, sparsity=0.9, r=32, seed=0,
-                 device="cuda"):
+                 device="cuda", around="torch"):
+        if around not in ("torch", "rola"):
+            raise ValueError(f'around must be "torch" or "rola", got {around!r}')
         self.s, self.attn, self.block, self.sparsity, self.r = shape, attn, block, sparsity, r
+        self.around = around
         d, H, dh = shape.d_model, shape.heads, shape.d_model // shape.heads
         assert dh == 128
         g = torch.Generator(device="cpu").manual_seed(seed)
@@ -82,6 +87,16 @@ class DiTBlock:
         self.ws_sp = torch.empty(R.sparse_combine_workspace_bytes(prob, block, sparsity, r),
                                  dtype=torch.uint8, device=device)
 
+    def _norm_mod(self, x, which):
+        """The modulated layer norm before the attention (0) or the MLP (1)."""
+        shift, scale = self.mod.float()[3 * which], self.mod.float()[3 * which + 1]
+        if self.around == "rola":
+            return R.rola_norm(x, 1 + scale, shift)[0]
+        return (_ln(x) * (1 + scale) + shift).to(x.dtype)
+
+    def _norm_qk(self, x, w):
+        return R.rola_norm(x, w, kind="rms")[0] if self.around == "rola" else _rms(x, w)
+
     def _heads(self, t):  # [N, d] -> [1, H, N, 128] contiguous
         N = t.shape[0]
         return t.view(N, self.s.heads, 128).transpose(0, 1).contiguous().unsqueeze(0)
@@ -91,7 +106,8 @@ class DiTBlock:
         s, g = self.s, self.s.grid
         qkv = h @ self.Wqkv.t() + self.bqkv
         q, k, v = qkv.split(s.d_model, dim=-1)
-        qn, kn, vh = self._heads(_rms(q, self.nq)), self._heads(_rms(k, self.nk)), self._heads(v)
+        qn, kn = self._heads(self._norm_qk(q, self.nq)), self._heads(self._norm_qk(k, self.nk))
+        vh = self._heads(v)
         qr = R.rola_rope_apply(qn, self.cos, self.sin, g)
         kr = R.rola_rope_apply(kn, self.cos, self.sin, g)
         if self.attn == "dense":
@@ -112,6 +128,12 @@ class DiTBlock:
 
     def cross_attention(self, x, ctx, chunk=8192):
         s = self.s
+        if self.around == "rola":
+            hc = R.rola_norm(x)[0]
+            q, k = self._norm_qk(hc @ self.Wcq.t(), self.ncq), self._norm_qk(ctx @ self.Wck.t(), self.nck)
+            heads = [t.view(1, -1, s.heads, 128).transpose(1, 2) for t in (q, k, ctx @ self.Wcv.t())]
+            o, _ = R.rola_attn(*heads, want_lse=False)
+            return o.transpose(1, 2).reshape(-1, s.d_model) @ self.Wco.t()
         hc = _ln(x).to(x.dtype)
         q = _rms(hc @ self.Wcq.t(), self.ncq).view(-1, s.heads, 128).transpose(0, 1).contiguous()
         kc = _rms(ctx @ self.Wck.t(), self.nck).view(-1, s.heads, 128).transpose(0, 1)
@@ -125,12 +147,12 @@ class DiTBlock:
 
     def forward(self, x, ctx, capture=None):
         """x: [N, d] hidden states, ctx: [L, d] text tokens (bf16) -> [N, d]."""
-        sh1, sc1, g1, sh2, sc2, g2 = self.mod.float()
-        h = (_ln(x) * (1 + sc1) + sh1).to(x.dtype)
+        _, _, g1, _, _, g2 = self.mod.float()
+        h = self._norm_mod(x, 0)
         a = self.self_attention(h, capture)
         x = (x.float() + g1 * (a @ self.Wo.t() + self.bo).float()).to(x.dtype)
         x = (x.float() + self.cross_attention(x, ctx).float()).to(x.dtype)
-        h2 = (_ln(x) * (1 + sc2) + sh2).to(x.dtype)
+        h2 = self._norm_mod(x, 1)
         f = F.gelu(h2 @ self.W1.t() + self.b1, approximate="tanh") @ self.W2.t() + self.b2
         return (x.float() + g2 * f.float()).to(x.dtype)
 

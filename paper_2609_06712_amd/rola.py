@@ -936,6 +936,10 @@ def _norm_rows(a, x, name, like=None):
     return ld
 
 
+def _rows_like(x):
+    return torch.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape)
+
+
 def _norm_params(a, x, w, name, dtype=None):
     """Groups of rows that a weight [d], or [B, d] for x [B, N, d], gives."""
     if not isinstance(w, torch.Tensor):
@@ -980,7 +984,7 @@ def rola_norm(X, W=None, Bias=None, kind="layer", eps=1e-6, out=None, want_stats
             raise ValueError("W and Bias must have the same shape")
         groups = gb
     if out is None:
-        out, ldy = torch.empty(X.shape, dtype=X.dtype, device=X.device), X.shape[-1]
+        out, ldy = _rows_like(X), X.shape[-1]
     else:
         ldy = _norm_rows(a, out, "out", X)
     a.done()
@@ -1019,7 +1023,7 @@ def rola_norm_backward(X, W, mean, rstd, dY, kind="layer", want_bias=True, per_s
         if name == "rstd" or kind == "layer":
             a.tensor(t, name, X.shape[:-1], torch.float32)
     if out is None:
-        out, ldo = torch.empty(X.shape, dtype=X.dtype, device=X.device), X.shape[-1]
+        out, ldo = _rows_like(X), X.shape[-1]
     else:
         ldo = _norm_rows(a, out, "out", X)
     key = _norm_key(X, W, groups, kind)
@@ -1052,44 +1056,79 @@ def _attn_ws(backward, *key):
     return fn(ctypes.byref(_attn_problem(*key)))
 
 
-def _in_place(a, x, name, shape, dtype):
+def _in_place(x, name, shape, dtype, device):
     """A [B, heads, N, d_h] tensor taken by its strides."""
     if not isinstance(x, torch.Tensor):
         raise ValueError(f"{name} must be a tensor")
-    if x.dtype != dtype:
-        raise ValueError(f"{name} must be {dtype}, got {x.dtype}")
-    if x.shape != shape and tuple(x.shape) != tuple(shape):
-        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(x.shape)}")
-    a.placed.append((x, name, True))
     s = x.stride()
+    if x.dtype != dtype or x.shape != shape or s[3] != 1 or x.get_device() != device or device < 0:
+        if x.dtype != dtype:
+            raise ValueError(f"{name} must be {dtype}, got {x.dtype}")
+        if x.shape != shape:
+            raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(x.shape)}")
+        if s[3] != 1:
+            raise ValueError(f"{name} must have a unit inner stride")
+        raise ValueError(f"{name} must be a device tensor" if device < 0 else
+                         f"{name} is on {x.device}, the other arguments on cuda:{device}")
     return Heads(x.data_ptr(), s[0], s[1], s[2])
 
 
-def _like_heads(x, shape=None):
+def _like_heads(x):
     """An output in x's order of heads and tokens: token after token (the heads of a token beside each
     other) where x has its heads inside its tokens, head after head otherwise."""
-    B, H, N, d = x.shape if shape is None else shape
-    if x.shape[1] > 1 and x.shape[2] > 1 and x.stride(1) < x.stride(2):
-        return torch.empty((B, N, H, d), dtype=x.dtype, device=x.device).transpose(1, 2)
-    return torch.empty((B, H, N, d), dtype=x.dtype, device=x.device)
+    if x.is_contiguous():
+        return torch.empty_like(x)
+    s = x.stride()
+    B, H, N, d = x.shape
+    if H > 1 and N > 1 and s[1] < s[2]:
+        if s == (N * H * d, d, H * d, 1):  # dense: kept as it is
+            return torch.empty_like(x)
+        return x.new_empty((B, N, H, d)).transpose(1, 2)
+    return x.new_empty((B, H, N, d))
 
 
-def _attn_args(a, Q, K, V, kv_len, causal):
+def _attn_args(Q, K, V, kv_len, causal):
     for t, name in ((Q, "Q"), (K, "K")):
         if not isinstance(t, torch.Tensor) or t.dim() != 4:
             raise ValueError(f"{name} must be a [B, heads, N, d_h] tensor")
-    if Q.dtype not in _ACT_DTYPES:
-        raise ValueError(f"Q must be bfloat16 or float32, got {Q.dtype}")
-    B, H, Nq, d = Q.shape
-    Hkv, Nk = K.shape[1], K.shape[2]
+    dtype, shape, device = Q.dtype, Q.shape, Q.get_device()
+    code = _DTYPE_CODES.get(dtype)
+    if code is None:
+        raise ValueError(f"Q must be bfloat16 or float32, got {dtype}")
+    B, H, Nq, d = shape
+    kshape = K.shape
+    _, Hkv, Nk, _ = kshape
     if Q.numel() == 0 or K.numel() == 0:
-        raise ValueError(f"empty tensors: Q {tuple(Q.shape)}, K {tuple(K.shape)}")
-    hq = _in_place(a, Q, "Q", Q.shape, Q.dtype)
-    hk = _in_place(a, K, "K", (B, Hkv, Nk, d), Q.dtype)
-    hv = _in_place(a, V, "V", (B, Hkv, Nk, d), Q.dtype)
+        raise ValueError(f"empty tensors: Q {tuple(shape)}, K {tuple(kshape)}")
+    if kshape[0] != B or kshape[3] != d:
+        raise ValueError(f"K must have shape {(B, Hkv, Nk, d)}, got {tuple(kshape)}")
+    hq = _in_place(Q, "Q", shape, dtype, device)
+    hk = _in_place(K, "K", kshape, dtype, device)
+    hv = _in_place(V, "V", kshape, dtype, device)
     if kv_len is not None:
-        a.tensor(kv_len, "kv_len", (B,), torch.int32)
-    return (B, H, Hkv, Nq, Nk, d, _DTYPE_CODES[Q.dtype], 1 if causal else 0), hq, hk, hv
+        _flat(kv_len, "kv_len", (B,), torch.int32, device)
+    return (B, H, Hkv, Nq, Nk, d, code, 1 if causal else 0), device, hq, hk, hv
+
+
+def _flat(x, name, shape, dtype, device):
+    """A contiguous tensor of a call whose other tensors are taken by their strides."""
+    a = _Args()
+    a.tensor(x, name, shape, dtype)
+    a.done()
+    if x.get_device() != device:
+        raise ValueError(f"{name} is on {x.device}, the other arguments on cuda:{device}")
+    return x
+
+
+def _attn_workspace(ws, need, Q, device):
+    if ws is None:
+        return torch.empty(need, dtype=torch.uint8, device=Q.device) if need else None
+    a = _Args()
+    a.workspace(ws)
+    a.done()
+    if ws.get_device() != device:
+        raise ValueError(f"ws is on {ws.device}, the other arguments on cuda:{device}")
+    return ws
 
 
 def attn_workspace_bytes(Q, K, causal=False, backward=False) -> int:
@@ -1106,24 +1145,18 @@ def rola_attn(Q, K, V, kv_len=None, causal=False, scale=None, out=None, lse=None
     j <= i + kv_len - Nq. Tensors are taken in place by their strides (unit inner stride), so views of packed
     projections need no copy; O comes in Q's order of heads and tokens. lse: fp32 [B, H, Nq], log2 of
     the softmax denominator of the log2e-scaled scores (None without want_lse)."""
-    a = _Args()
-    key, hq, hk, hv = _attn_args(a, Q, K, V, kv_len, causal)
+    key, device, hq, hk, hv = _attn_args(Q, K, V, kv_len, causal)
     if out is None:
         out = _like_heads(Q)
-    ho = _in_place(a, out, "out", Q.shape, Q.dtype)
+    ho = _in_place(out, "out", Q.shape, Q.dtype, device)
     if lse is not None:
-        a.tensor(lse, "lse", Q.shape[:3], torch.float32)
+        _flat(lse, "lse", Q.shape[:3], torch.float32, device)
     elif want_lse:
-        lse = torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device)
-    need = _attn_ws(False, *key)
-    if ws is None and need:
-        ws = torch.empty(need, dtype=torch.uint8, device=Q.device)
-    a.workspace(ws)
-    a.done()
-    st = _stream_here(Q, stream)
-    _check(LIB.rola_attn(_attn_problem(*key), hq, hk, hv, _ptr(kv_len),
-                         key[5] ** -0.5 if scale is None else scale, ho, _ptr(lse), _ptr(ws),
-                         0 if ws is None else ws.numel(), st), "rola_attn")
+        lse = Q.new_empty(Q.shape[:3], dtype=torch.float32)
+    ws = _attn_workspace(ws, _attn_ws(False, *key), Q, device)
+    _check(LIB.rola_attn(_attn_problem(*key), hq, hk, hv, _ptr(kv_len), key[5] ** -0.5 if scale is None else scale,
+                         ho, _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel(), _stream_here(Q, stream)),
+           "rola_attn")
     return out, lse
 
 
@@ -1131,23 +1164,20 @@ def rola_attn_backward(Q, K, V, O, lse, dO, kv_len=None, causal=False, scale=Non
                        ws=None, stream=None):
     """(dQ, dK, dV) of rola_attn in the inputs' type, from its O and lse; kv_len, causal and scale as in
     the forward. Outputs come in the order of heads and tokens of Q, K and V, or are the tensors given."""
-    a = _Args()
-    key, hq, hk, hv = _attn_args(a, Q, K, V, kv_len, causal)
-    ho = _in_place(a, O, "O", Q.shape, Q.dtype)
-    hg = _in_place(a, dO, "dO", Q.shape, Q.dtype)
-    a.tensor(lse, "lse", Q.shape[:3], torch.float32)
+    key, device, hq, hk, hv = _attn_args(Q, K, V, kv_len, causal)
+    shape, kshape, dtype = Q.shape, K.shape, Q.dtype
+    ho = _in_place(O, "O", shape, dtype, device)
+    hg = _in_place(dO, "dO", shape, dtype, device)
+    _flat(lse, "lse", shape[:3], torch.float32, device)
     dQ = _like_heads(Q) if dQ is None else dQ
     dK = _like_heads(K) if dK is None else dK
     dV = _like_heads(V) if dV is None else dV
-    gq = _in_place(a, dQ, "dQ", Q.shape, Q.dtype)
-    gk = _in_place(a, dK, "dK", K.shape, Q.dtype)
-    gv = _in_place(a, dV, "dV", K.shape, Q.dtype)
-    if ws is None:
-        ws = torch.empty(_attn_ws(True, *key), dtype=torch.uint8, device=Q.device)
-    a.workspace(ws)
-    a.done()
-    st = _stream_here(Q, stream)
+    gq = _in_place(dQ, "dQ", shape, dtype, device)
+    gk = _in_place(dK, "dK", kshape, dtype, device)
+    gv = _in_place(dV, "dV", kshape, dtype, device)
+    ws = _attn_workspace(ws, _attn_ws(True, *key), Q, device)
     _check(LIB.rola_attn_backward(_attn_problem(*key), hq, hk, hv, _ptr(kv_len),
-                                  key[5] ** -0.5 if scale is None else scale, ho, _ptr(lse), hg, gq, gk, gv,
-                                  _ptr(ws), ws.numel(), st), "rola_attn_backward")
+                                  key[5] ** -0.5 if scale is None else scale, ho, lse.data_ptr(), hg, gq, gk, gv,
+                                  _ptr(ws), 0 if ws is None else ws.numel(), _stream_here(Q, stream)),
+           "rola_attn_backward")
     return dQ, dK, dV

@@ -6,6 +6,10 @@ O^s with its per-query log-sum-exp, and the summary C. backward() runs the low-r
 (which also yields dO^s and the gate-logit gradient), the block-sparse attention backward, and maps
 dQ^r, dK^r back through the backbone rotation (R(p)^T = R(-p)); the two branches' shares of dQ^n,
 dK^n and dV are added. Every step, the additions included, runs in the library's kernels.
+
+cross_forward() and cross_backward() do the same for the block's text cross-attention beside the module: layer
+norm of the hidden states, projections (library GEMMs), RMS norm of q and k, attention over each sample's text
+tokens, output projection. q, k, v and their gradients stay views of the projections' rows: nothing is transposed.
 """
 
 from __future__ import annotations
@@ -42,3 +46,52 @@ def backward(Qn, Kn, V, Pq, Pk, logits, saved, dO):
                                            saved["sparsity"], saved["idx"], saved["os"], saved["lse"],
                                            dOs, cos, sin, dQn, dKn, dV)
     return dict(dQn=dQn, dKn=dKn, dV=dV, dPq=dPq, dPk=dPk, dlogits=dlog)
+
+
+def cross_forward(x, ctx, w, heads, kv_len=None, eps=1e-6):
+    """Text cross-attention: x [B, N, d] hidden states, ctx [B, L, d] text tokens, kv_len (int32 [B], on the
+    device) the valid ones per sample. w: dict of the layer norm's ln_w, ln_b ([d], or [B, d] per sample;
+    None for neither), the projections Wq, Wk, Wv, Wo [d, d] and the RMS norms' nq, nk [d]. Returns
+    (out [B, N, d], what cross_backward takes)."""
+    B, N, d = x.shape
+    L = ctx.shape[1]
+    h, mean, rstd = R.rola_norm(x, w["ln_w"], w["ln_b"], kind="layer", eps=eps, want_stats=True)
+    q0, k0, v = h @ w["Wq"].t(), ctx @ w["Wk"].t(), ctx @ w["Wv"].t()
+    qn, _, rq = R.rola_norm(q0, w["nq"], kind="rms", eps=eps, want_stats=True)
+    kn, _, rk = R.rola_norm(k0, w["nk"], kind="rms", eps=eps, want_stats=True)
+    q, k, vh = (t.view(B, n, heads, d // heads).transpose(1, 2) for t, n in ((qn, N), (kn, L), (v, L)))
+    o, lse = R.rola_attn(q, k, vh, kv_len=kv_len)
+    out = o.transpose(1, 2).reshape(B, N, d) @ w["Wo"].t()
+    saved = dict(h=h, mean=mean, rstd=rstd, q0=q0, k0=k0, rq=rq, rk=rk, q=q, k=k, v=vh, o=o, lse=lse,
+                 kv_len=kv_len)
+    return out, saved
+
+
+def cross_backward(x, ctx, w, saved, dout):
+    """Gradients of <dout, out>: dict of dx, dctx in the inputs' type, the projections' dWq, dWk, dWv, dWo in
+    theirs, and the norms' dln_w, dln_b, dnq, dnk in fp32."""
+    s = saved
+    B, N, d = x.shape
+
+    def rows(t):
+        return t.reshape(-1, t.shape[-1])
+
+    def merged(t):  # [B, heads, n, d_h] -> [B, n, d], a view when the heads lie inside the tokens
+        return t.transpose(1, 2).reshape(B, t.shape[2], d)
+
+    g = {}
+    heads = s["q"].shape[1]
+    g["dWo"] = rows(dout).t() @ rows(merged(s["o"]))
+    do = (dout @ w["Wo"]).view(B, N, heads, d // heads).transpose(1, 2)
+    dq, dk, dv = R.rola_attn_backward(s["q"], s["k"], s["v"], s["o"], s["lse"], do, kv_len=s["kv_len"])
+    dq0, g["dnq"], _ = R.rola_norm_backward(s["q0"], w["nq"], None, s["rq"], merged(dq), kind="rms",
+                                            want_bias=False)
+    dk0, g["dnk"], _ = R.rola_norm_backward(s["k0"], w["nk"], None, s["rk"], merged(dk), kind="rms",
+                                            want_bias=False)
+    dv = merged(dv)
+    g["dWq"], g["dWk"], g["dWv"] = (rows(a).t() @ rows(b) for a, b in ((dq0, s["h"]), (dk0, ctx), (dv, ctx)))
+    g["dctx"] = dk0 @ w["Wk"] + dv @ w["Wv"]
+    per_sample = w["ln_w"] is not None and w["ln_w"].dim() == 2
+    g["dx"], g["dln_w"], g["dln_b"] = R.rola_norm_backward(x, w["ln_w"], s["mean"], s["rstd"], dq0 @ w["Wq"],
+                                                           kind="layer", per_sample=per_sample)
+    return g
