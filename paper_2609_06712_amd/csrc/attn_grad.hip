@@ -25,7 +25,16 @@ namespace {
 
 constexpr int kRows = 32;            // rows of a sub-tile
 constexpr int kTile = kRows * 256;   // its bytes (bf16, d 128)
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ uint32_t pair_bf16(float a, float b) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, bf16x2{(bf16)a, (bf16)b});
+}
+__device__ __forceinline__ uint32_t pair_f16(float a, float b) {
+  return __builtin_bit_cast(uint32_t, f16x2{(_Float16)a, (_Float16)b});
+}
 
 struct GradArgs {
   AttnCall c;     // c.O: dO
@@ -522,7 +531,7 @@ __device__ __forceinline__ Walk walk_of(const GradArgs& a, int n, int key0, cons
 // rounding to bf16 that dS takes next). A wave has its SIMD to itself: two 32-key tiles, so that what it reads
 // from LDS serves two products (one tile per wave and two waves per SIMD read 1.5 times what the LDS delivers
 // while the products run), and the softmax of one tile lies between the products of the other:
-//   S_0 | S_1 with P_0 | dV_0 with P_1 | dV_1 with the next step's row operand.
+//   S_0 | S_1 with P_0 | dV_0 with P_1 and the next step's row operand | dV_1.
 constexpr int kDkvBuf = 5;
 template <bool CAUSAL>
 __global__ __launch_bounds__(256, 1) void attn_dkv_bf16_kernel(const GradArgs a) {
@@ -565,33 +574,37 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_bf16_kernel(const GradArgs a)
   }
   const uint32_t lds0 = lds_address(lds);
   const uint32_t dst0 = lds0 + role * kTile + kw * DPW * 1024;
-  const char* mbase = (role ? c.O.p + pt.b * c.O.b : c.Q.p + pt.b * c.Q.b) + (long)pt.hk * c.G * hstride;
-  const char* sbase = reinterpret_cast<const char*>(a.stat + ((long)pt.b * a.H + (long)pt.hk * c.G) * a.Np * 2);
-  int ig = 0, iq = wk.q0, cq = wk.q0;  // the next step to load; the query of the next step to take
-  if (wk.tiles > 0) {
-    ig = wk.t0 / wk.tiles;
-    iq = cq = wk.q0 + wk.t0 % wk.tiles * 32;
-  }
-  int issued = 0, ibuf = 0;
+  // The next step to load: its first query, its rows and statistics (pointers that move with it), its stage.
+  const int g0 = wk.tiles > 0 ? wk.t0 / wk.tiles : 0, i0 = wk.q0 + (wk.t0 - g0 * wk.tiles) * 32;
+  const char* rows = (role ? c.O.p + pt.b * c.O.b : c.Q.p + pt.b * c.Q.b) + ((long)pt.hk * c.G + g0) * hstride +
+                     i0 * nstride;
+  const char* stats = reinterpret_cast<const char*>(a.stat + (((long)pt.b * a.H + (long)pt.hk * c.G + g0) * a.Np + i0) * 2);
+  const long rstep = 32 * nstride, rhead = hstride - (wk.tiles - 1) * rstep;  // to the next tile, the next head's first
+  const int shead = 8 * a.Np - (wk.tiles - 1) * 256;
+  int iq = i0, cq = i0, issued = 0;  // cq: the query of the next step to take
+  uint32_t dst = dst0, sdst = lds0 + 2 * kTile;
+  const uint32_t dst_end = dst0 + NBUF * STAGE;
   auto issue = [&]() {
-    const char* base = mbase + ig * hstride + (long)iq * nstride;
-    const uint32_t dst = dst0 + ibuf * STAGE;
     if (iq + 32 <= c.Nq) {
 #pragma unroll
-      for (int x = 0; x < DPW; ++x) dma16(base, dsrc[x], dst + x * 1024);
+      for (int x = 0; x < DPW; ++x) dma16(rows, dsrc[x], dst + x * 1024);
     } else {  // rows past the last query re-read it (P = 0 there)
 #pragma unroll
       for (int x = 0; x < DPW; ++x) {
         const int back = max(4 * (kw * DPW + x) + lane / 16 - (c.Nq - 1 - iq), 0);
-        dma16(base, dsrc[x] - back * (uint32_t)nstride, dst + x * 1024);
+        dma16(rows, dsrc[x] - back * (uint32_t)nstride, dst + x * 1024);
       }
     }
     // lse, D of the 32 queries (256 bytes; lanes 16-63 repeat lanes 0-15)
-    if (wave == 0) dma16(sbase + ((long)ig * a.Np + iq) * 8, (lane % 16) * 16, lds0 + ibuf * STAGE + 2 * kTile);
+    if (wave == 0) dma16(stats, (lane % 16) * 16, sdst);
     iq += 32;
-    if (iq >= c.Nq) iq = wk.q0, ++ig;
+    const bool head_end = iq >= c.Nq;
+    rows += head_end ? rhead : rstep;
+    stats += head_end ? shead : 256;
+    iq = head_end ? wk.q0 : iq;
+    dst += STAGE, sdst += STAGE;
+    if (dst == dst_end) dst -= NBUF * STAGE, sdst -= NBUF * STAGE;
     ++issued;
-    if (++ibuf == NBUF) ibuf = 0;
   };
 
   char* pbase = lds + NBUF * STAGE + kw * 4096 + lane * 16;  // + buffer * PBUF + tile * 2048 + half * 1024
@@ -637,21 +650,28 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_bf16_kernel(const GradArgs a)
       const char* next = lds + (ROLE ? buf : ahead) * STAGE + ROLE * kTile;  // the next step's rows
       bf16x8 fb[8];
       float lv[16];  // lse (role 0) or D (role 1) of the step's queries 8 (k / 4) + 4 hh + k % 4
-      f16x8 ph[2][2];
+      uint32_t ph[2][8], b2[2][8];  // pairs of fp16 P; of bf16 P or dS
       f32x16 X[2] = {f32x16{}, f32x16{}};
-      bf16x8 b2[2][2];
-      // P or dS of two queries of tile u
+      // P or dS of the queries k, k + 1 of tile u. (The empty assembly keeps the work where it stands: the compiler
+      // would otherwise sink it past the products it is to lie between.)
       auto middle = [&](int u, int k) {
         if constexpr (ROLE == 0) {
           const float p = __builtin_amdgcn_exp2f(fmaf(X[u][k], c.scale_log2, -lv[k]));
           const float q = __builtin_amdgcn_exp2f(fmaf(X[u][k + 1], c.scale_log2, -lv[k + 1]));
-          b2[u][k / 8][k % 8] = (bf16)p, b2[u][k / 8][k % 8 + 1] = (bf16)q;
-          ph[u][k / 8][k % 8] = (_Float16)p, ph[u][k / 8][k % 8 + 1] = (_Float16)q;
-          if (k % 8 == 6) *reinterpret_cast<f16x8*>(pb + u * 2048 + k / 8 * 1024) = ph[u][k / 8];
+          b2[u][k / 2] = pair_bf16(p, q);
+          ph[u][k / 2] = pair_f16(p, q);
+          asm volatile("" : "+v"(b2[u][k / 2]), "+v"(ph[u][k / 2]));
+          if (k % 8 == 6)
+            *reinterpret_cast<uint4*>(pb + u * 2048 + k / 8 * 1024) =
+                make_uint4(ph[u][k / 2 - 3], ph[u][k / 2 - 2], ph[u][k / 2 - 1], ph[u][k / 2]);
         } else {
-          b2[u][k / 8][k % 8] = (bf16)((float)ph[u][k / 8][k % 8] * (X[u][k] - lv[k]));
-          b2[u][k / 8][k % 8 + 1] = (bf16)((float)ph[u][k / 8][k % 8 + 1] * (X[u][k + 1] - lv[k + 1]));
+          const f16x2 p = __builtin_bit_cast(f16x2, ph[u][k / 2]);
+          b2[u][k / 2] = pair_bf16((float)p[0] * (X[u][k] - lv[k]), (float)p[1] * (X[u][k + 1] - lv[k + 1]));
+          asm volatile("" : "+v"(b2[u][k / 2]));
         }
+      };
+      auto operand = [&](int u, int v) {
+        return __builtin_bit_cast(bf16x8, u32x4{b2[u][4 * v], b2[u][4 * v + 1], b2[u][4 * v + 2], b2[u][4 * v + 3]});
       };
       auto hide = [&](int u) {  // P = 0 where the query is before the key
         if (CAUSAL && ROLE == 0 && key0 + kw * 64 + 32 * u + 31 > cq + off) {
@@ -669,10 +689,15 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_bf16_kernel(const GradArgs a)
           const float4 v = *reinterpret_cast<const float4*>(stage + 2 * kTile + ROLE * 128 + 32 * s + 16 * hh);
           lv[4 * s] = v.x, lv[4 * s + 1] = v.y, lv[4 * s + 2] = v.z, lv[4 * s + 3] = v.w;
         } else if (ROLE == 1) {
-          ph[s / 2 - 2][s % 2] = *reinterpret_cast<const f16x8*>(pb + (s / 2 - 2) * 2048 + s % 2 * 1024);
+          const uint4 v = *reinterpret_cast<const uint4*>(pb + (s / 2 - 2) * 2048 + s % 2 * 1024);
+        uint32_t* at = &ph[s / 2 - 2][4 * (s % 2)];
+        at[0] = v.x, at[1] = v.y, at[2] = v.z, at[3] = v.w;
         }
         __builtin_amdgcn_sched_barrier(0);
       }
+      // (all accumulators at once in their register file: the compiler moved one out and back to make room for S)
+      asm volatile("" : "+a"(acc[0][0]), "+a"(acc[0][1]), "+a"(acc[0][2]), "+a"(acc[0][3]), "+a"(acc[1][0]),
+                        "+a"(acc[1][1]), "+a"(acc[1][2]), "+a"(acc[1][3]), "+a"(X[0]));
       hide(0);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -685,14 +710,14 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_bf16_kernel(const GradArgs a)
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int s = 0; s < 8; ++s) {
-        acc[0][s % 4] = mfma_bf16(fb[2 * (s % 4) + s / 4], b2[0][s / 4], acc[0][s % 4]);
+        acc[0][s % 4] = mfma_bf16(fb[2 * (s % 4) + s / 4], operand(0, s / 4), acc[0][s % 4]);
         middle(1, 2 * s);
+        fa[s] = row_frag(next, lane % 32, s, hh);
         __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
       for (int s = 0; s < 8; ++s) {
-        acc[1][s % 4] = mfma_bf16(fb[2 * (s % 4) + s / 4], b2[1][s / 4], acc[1][s % 4]);
-        fa[s] = row_frag(next, lane % 32, s, hh);
+        acc[1][s % 4] = mfma_bf16(fb[2 * (s % 4) + s / 4], operand(1, s / 4), acc[1][s % 4]);
         __builtin_amdgcn_sched_barrier(0);
       }
       cq += 32;
