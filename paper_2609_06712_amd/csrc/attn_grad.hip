@@ -584,37 +584,47 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_bf16_kernel(const GradArgs a)
   int iq = i0, cq = i0, issued = 0;  // cq: the query of the next step to take
   uint32_t dst = dst0, sdst = lds0 + 2 * kTile;
   const uint32_t dst_end = dst0 + NBUF * STAGE;
-  auto issue = [&]() {
-    if (iq + 32 <= c.Nq) {
+  uint32_t from[DPW];
+  auto aim = [&]() {
 #pragma unroll
-      for (int x = 0; x < DPW; ++x) dma16(rows, dsrc[x], dst + x * 1024);
-    } else {  // rows past the last query re-read it (P = 0 there)
+    for (int x = 0; x < DPW; ++x) from[x] = dsrc[x];
+    if (iq + 32 > c.Nq) {  // rows past the last query re-read it (P = 0 there)
 #pragma unroll
-      for (int x = 0; x < DPW; ++x) {
-        const int back = max(4 * (kw * DPW + x) + lane / 16 - (c.Nq - 1 - iq), 0);
-        dma16(rows, dsrc[x] - back * (uint32_t)nstride, dst + x * 1024);
-      }
+      for (int x = 0; x < DPW; ++x)
+        from[x] -= max(4 * (kw * DPW + x) + lane / 16 - (c.Nq - 1 - iq), 0) * (uint32_t)nstride;
     }
-    // lse, D of the 32 queries (256 bytes; lanes 16-63 repeat lanes 0-15)
+  };
+  auto load = [&](int x) { dma16(rows, from[x], dst + x * 1024); };
+  auto load_stats = [&]() {  // lse, D of the 32 queries (256 bytes; lanes 16-63 repeat lanes 0-15)
     if (wave == 0) dma16(stats, (lane % 16) * 16, sdst);
+  };
+  auto loaded = [&]() {  // on to the next step; past the last it is loaded again, to stages that nothing reads
+    dst += STAGE, sdst += STAGE;
+    if (dst == dst_end) dst -= NBUF * STAGE, sdst -= NBUF * STAGE;
+    if (++issued >= T) return;
     iq += 32;
     const bool head_end = iq >= c.Nq;
     rows += head_end ? rhead : rstep;
     stats += head_end ? shead : 256;
     iq = head_end ? wk.q0 : iq;
-    dst += STAGE, sdst += STAGE;
-    if (dst == dst_end) dst -= NBUF * STAGE, sdst -= NBUF * STAGE;
-    ++issued;
+  };
+  auto issue = [&]() {
+    aim();
+#pragma unroll
+    for (int x = 0; x < DPW; ++x) load(x);
+    load_stats();
+    loaded();
   };
 
   char* pbase = lds + NBUF * STAGE + kw * 4096 + lane * 16;  // + buffer * PBUF + tile * 2048 + half * 1024
+  if (T > 0) {
 #pragma unroll
-  for (int j = 0; j < NBUF - 2; ++j)
-    if (j < T) issue();
-  wait_vm<0>();
-  __syncthreads();
+    for (int j = 0; j < NBUF - 2; ++j) issue();
+    wait_vm<0>();
+    __syncthreads();
+  }
   // Iteration t: role 0 takes step t, role 1 step t - 1; the row operand of the step after is read in both. The
-  // loads of step t + NBUF - 2 go where role 1 was one iteration ago.
+  // waves meet before its last products: the loads of step t + NBUF - 1 go where role 1 was in it.
   auto walk = [&](auto role_tag) {
     constexpr int ROLE = decltype(role_tag)::value;
     bf16x8 fa[8];
@@ -623,26 +633,26 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_bf16_kernel(const GradArgs a)
       for (int s = 0; s < 8; ++s) fa[s] = row_frag(tile, lane % 32, s, hh);
     };
     int buf = 0, back = NBUF - 1;  // stages of steps t and t - 1
-    auto arrive = [&](int t) {
-      if (issued >= t + 3)  // stage t + 1 has landed; one more step's loads may be under way
-        wait_vm<DPW>();
-      else
-        wait_vm<0>();
+    auto meet = [&]() {  // the stage after the next has landed; one more step's loads may be under way
+      wait_vm<DPW>();
       __syncthreads();
-      if (issued < T) issue();
+    };
+    auto arrive = [&]() {
+      meet();
+      issue();
     };
     auto advance = [&]() {
       back = buf;
       buf = buf + 1 == NBUF ? 0 : buf + 1;
     };
+    arrive();
     if (ROLE == 1) {
-      arrive(0);
       advance();
+      arrive();
     }
     row_operands(lds + ROLE * kTile);
     // (one straight body per role: with a test around it the accumulators move between register files)
     for (int t = ROLE; t < T + ROLE; ++t) {
-      arrive(t);
       const int ahead = buf + 1 == NBUF ? 0 : buf + 1;
       const char* stage = lds + (ROLE ? back : buf) * STAGE;
       char* pb = pbase + ((t - ROLE) & 1) * PBUF;
@@ -715,16 +725,23 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_bf16_kernel(const GradArgs a)
         fa[s] = row_frag(next, lane % 32, s, hh);
         __builtin_amdgcn_sched_barrier(0);
       }
+      // the last products, with the next loads between them
+      aim();
+      meet();
 #pragma unroll
       for (int s = 0; s < 8; ++s) {
         acc[1][s % 4] = mfma_bf16(fb[2 * (s % 4) + s / 4], operand(1, s / 4), acc[1][s % 4]);
+        if (s < DPW) load(s);
+        if (s == DPW) load_stats();
+        if (s == DPW + 1) loaded();
         __builtin_amdgcn_sched_barrier(0);
       }
       cq += 32;
       if (cq >= c.Nq) cq = wk.q0;
       advance();
     }
-    if (ROLE == 0) arrive(T);
+    if (ROLE == 0) arrive();
+    wait_vm<0>();  // (loads still under way write to this workgroup's LDS)
   };
   if (T > 0) {
     if (role)
