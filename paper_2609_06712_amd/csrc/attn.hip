@@ -65,9 +65,8 @@ __global__ __launch_bounds__(256, QW == 4 ? 3 : 1) void attn_bf16_kernel(const F
   const int wave = wave_uniform(threadIdx.x / 64), lane = threadIdx.x % 64, hh = lane / 32;
   const int n = attn_keys(c, pt.b);
   const int row0 = (pt.tile * QW + (QW == 4 ? wave : 0)) * 32;  // first row of this wave
-  const int r = min(row0 + lane % 32, a.R - 1), i = r / c.G, g = r % c.G;
-  const bool rvalid = row0 + lane % 32 < a.R;
-  const int lim = attn_limit(c, n, i);
+  const int r = min(row0 + lane % 32, a.R - 1);
+  const int lim = attn_limit(c, n, r / c.G);
   // least and greatest limit of the wave's rows, and the greatest of the workgroup's
   const int lim_lo = attn_limit(c, n, min(row0, a.R - 1) / c.G);
   const int lim_hi = row0 < a.R ? attn_limit(c, n, min(row0 + 31, a.R - 1) / c.G) : 0;
@@ -92,11 +91,11 @@ __global__ __launch_bounds__(256, QW == 4 ? 3 : 1) void attn_bf16_kernel(const F
 
   bf16x8 qf[8];
   {
-    const char* q = c.Q.p + pt.b * c.Q.b + (pt.hk * c.G + g) * c.Q.h + i * c.Q.n;
+    const char* q = row_at(row_base(c.Q, pt.b, pt.hk, c.G), r);
 #pragma unroll
     for (int s = 0; s < 8; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(q + 32 * s + 16 * hh);
+    wait_vm<0>();
   }
-  wait_vm<0>();
 
   int vo[4];
   f32x16 acc[4];
@@ -245,27 +244,20 @@ __global__ __launch_bounds__(256, QW == 4 ? 3 : 1) void attn_bf16_kernel(const F
     store8(out + 8, o + 8);
     if (a.lse && c0 == 0)
       a.lse[(pt.b * a.heads + head) * c.Nq + ii] = sum > 0.f ? mx + __log2f(sum) : -__builtin_inff();
-  } else if (rvalid) {
+  } else {
     if (pt.left >= 0) {
       const long at = ((long)pt.left * pt.splits + pt.split) * 128 + wave * 32 + lane % 32;
+      if (row0 + lane % 32 >= a.R) return;
       store_grad_row<false>(a.part + at * D, acc, 1.f, hh, nullptr, nullptr);
       if (hh == 0) a.ml[at] = make_float2(m, l);
       return;
     }
-    const int head = pt.hk * c.G + g;
-    const float f = l > 0.f ? 1.f / l : 0.f;
-    char* out = c.O.p + pt.b * c.O.b + head * c.O.h + i * c.O.n;
-#pragma unroll
-    for (int w = 0; w < 4; ++w)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        bf16x4 o;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = (bf16)(acc[w][4 * j + e] * f);
-        *reinterpret_cast<bf16x4*>(out + 2 * (32 * w + 8 * j + 4 * hh)) = o;
-      }
-    if (a.lse && hh == 0)
-      a.lse[(pt.b * a.heads + head) * c.Nq + i] = l > 0.f ? m + __log2f(l) : -__builtin_inff();
+    __syncthreads();  // every wave is done with the stages
+    rows_from_acc(lds + wave * 8192, acc, l > 0.f ? 1.f / l : 0.f, row_base(c.O, pt.b, pt.hk, c.G), row0, a.R, lane);
+    int q = row0 + lane % 32;
+    asm volatile("" : "+v"(q));  // (divided again here, or the first quotient stays in a register all the way)
+    if (a.lse && hh == 0 && q < a.R)
+      a.lse[(pt.b * a.heads + pt.hk * c.G + q % c.G) * c.Nq + q / c.G] = l > 0.f ? m + __log2f(l) : -__builtin_inff();
   }
 }
 

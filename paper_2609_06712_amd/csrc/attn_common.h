@@ -122,6 +122,46 @@ inline Cut make_cut(int tiles, int bh, bool causal, int slots, int steps, double
 inline bool f32_few(long tiles, long bh) { return tiles * bh < 2 * kCus; }
 inline long cut_left(const Cut& c) { return c.splits > 1 ? (c.total - c.whole) / c.splits : 0; }
 
+// Query head rows of one (b, key head): row r is query r / G of head hk G + r % G.
+struct RowBase {
+  char* p;  // query 0 of the first head
+  long h, n;
+  int G;
+};
+__device__ __forceinline__ RowBase row_base(const View& v, int b, int hk, int G) {
+  return RowBase{v.p + b * v.b + (long)hk * G * v.h, v.h, v.n, G};
+}
+__device__ __forceinline__ char* row_at(const RowBase& v, int r) {
+  if (v.G == 1) return v.p + (long)r * v.n;  // (uniform; a division costs twenty instructions)
+  const int i = r / v.G;
+  return v.p + (long)i * v.n + (long)(r - i * v.G) * v.h;
+}
+
+// Stores the wave's 32 rows from the accumulator layout of a 32x32 tile set (lane: row l%32, channels
+// 32 w + 8 j + 4 hh ..), scaled by f and rounded to bf16, through 8 KB of LDS of its own: whole rows of 256
+// bytes, four to a store, instead of 16-byte pieces of 32 rows (text cross-attention of 2 x 32760 queries, 512 and
+// 73 keys: forward 235 -> 219 us).
+__device__ __forceinline__ void rows_from_acc(char* tile, const f32x16 (&acc)[4], float f, const RowBase& v,
+                                              int row0, int rows, int lane) {
+  const int hh = lane / 32, own = lane % 32;
+#pragma unroll
+  for (int w = 0; w < 4; ++w)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      bf16x4 o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = (bf16)(acc[w][4 * j + e] * f);
+      *reinterpret_cast<bf16x4*>(tile + own * 256 + (((4 * w + j) ^ bw_swizzle(own)) << 4) + 8 * hh) = o;
+    }
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int x = 0; x < 8; ++x) {
+    const int row = 4 * x + lane / 16, c = lane % 16;
+    const uint4 o = *reinterpret_cast<const uint4*>(tile + row * 256 + ((c ^ bw_swizzle(row)) << 4));
+    if (row0 + row < rows) *reinterpret_cast<uint4*>(row_at(v, row0 + row) + 16 * c) = o;
+  }
+}
+
 // s_waitcnt vmcnt(N), the other counters free.
 template <int N>
 __device__ __forceinline__ void wait_vm() {

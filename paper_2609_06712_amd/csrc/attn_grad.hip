@@ -105,19 +105,6 @@ __global__ __launch_bounds__(256) void attn_rowdot_f32_kernel(int H, int Nq, int
 
 // ---- dQ ------------------------------------------------------------------------------------------------
 
-// Stores 128 channels of a row from the accumulator layout of a 32x32 tile set, rounded to bf16.
-__device__ __forceinline__ void store_row_bf16(char* row, const f32x16 (&acc)[4], float f, int hh) {
-#pragma unroll
-  for (int w = 0; w < 4; ++w)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      bf16x4 o;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = (bf16)(acc[w][4 * j + e] * f);
-      *reinterpret_cast<bf16x4*>(row + 2 * (32 * w + 8 * j + 4 * hh)) = o;
-    }
-}
-
 // D = rowsum(P dP): four waves of 64 rows walk the keys in sub-tiles of 32 through three LDS stages. Two row
 // tiles per wave: an operand read from LDS serves two products, and without a gradient's accumulators two
 // workgroups fit a CU.
@@ -378,12 +365,14 @@ __global__ __launch_bounds__(256, 2) void attn_dq_bf16_kernel(const GradArgs a) 
       ++t;
     }
   }
-  if (row0 + lane % 32 >= a.R) return;
-  if (pt.left >= 0)
-    store_grad_row<false>(a.part + (((long)pt.left * pt.splits + pt.split) * 128 + wave * 32 + lane % 32) * 128, acc,
-                          c.scale, hh, nullptr, nullptr);
-  else
-    store_row_bf16(a.G1.p + pt.b * a.G1.b + head * a.G1.h + i * a.G1.n, acc, c.scale, hh);
+  if (pt.left >= 0) {
+    if (row0 + lane % 32 < a.R)
+      store_grad_row<false>(a.part + (((long)pt.left * pt.splits + pt.split) * 128 + wave * 32 + lane % 32) * 128, acc,
+                            c.scale, hh, nullptr, nullptr);
+    return;
+  }
+  __syncthreads();  // every wave is done with the stages
+  rows_from_acc(lds + wave * 8192, acc, c.scale, row_base(a.G1, pt.b, pt.hk, c.G), row0, a.R, lane);
 }
 
 // fp32: four waves of 16 rows, key tiles of 32 staged in LDS.
@@ -749,21 +738,23 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_bf16_kernel(const GradArgs a)
     else
       walk(std::integral_constant<int, 0>{});
   }
+  __syncthreads();  // every wave is done with the stages
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     const int k = key + 32 * u;
-    if (k >= c.Nk) break;
     if (k >= n) {  // a key that is not there (its column holds the last one's)
 #pragma unroll
       for (int w = 0; w < 4; ++w) acc[u][w] = f32x16{};
     }
     const float f = role ? c.scale : 1.f;
     if (pt.left >= 0) {
+      if (k >= c.Nk) break;
       float* out = a.part + (role ? 0 : a.part2) + (((long)pt.left * pt.splits + pt.split) * 128 + k - key0) * 128;
       store_grad_row<false>(out, acc[u], f, hh, nullptr, nullptr);
     } else {
       const View& g = role ? a.G1 : a.G2;
-      store_row_bf16(g.p + pt.b * g.b + pt.hk * g.h + k * g.n, acc[u], f, hh);
+      rows_from_acc(lds + wave * 8192, acc[u], f, RowBase{g.p + pt.b * g.b + pt.hk * g.h, 0, g.n, 1},
+                    key0 + kw * 64 + 32 * u, c.Nk, lane);
     }
   }
 }
