@@ -314,6 +314,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_bf16_kernel(const GradArgs a) 
         const char* Vt = Kt + kTile;
         bf16x8 ka[8], va[8], kt[8];
         f32x16 sc = f32x16{}, dp = f32x16{};
+        __builtin_amdgcn_s_setprio(0);
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
           ka[s] = row_frag(Kt, lane % 32, s, hh);
@@ -340,6 +341,8 @@ __global__ __launch_bounds__(256, 2) void attn_dq_bf16_kernel(const GradArgs a) 
           for (int k = 0; k < 16; ++k) sc[k] = 8 * (k / 4) + k % 4 < left ? sc[k] : -__builtin_inff();
         }
         __builtin_amdgcn_sched_barrier(0);
+        // ahead of the other workgroup's scores: 8400 tokens, 12 heads 763 -> 735 us
+        __builtin_amdgcn_s_setprio(1);
         bf16x8 ds[2], dl[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
