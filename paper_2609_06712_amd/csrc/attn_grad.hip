@@ -572,7 +572,7 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_bf16_kernel(const GradArgs a)
                      i0 * nstride;
   const char* stats = reinterpret_cast<const char*>(a.stat + (((long)pt.b * a.H + (long)pt.hk * c.G + g0) * a.Np + i0) * 2);
   const long rstep = 32 * nstride, rhead = hstride - (wk.tiles - 1) * rstep;  // to the next tile, the next head's first
-  const int shead = 8 * a.Np - (wk.tiles - 1) * 256;
+  const long shead = 8L * a.Np - (wk.tiles - 1) * 256L;
   int iq = i0, cq = i0, issued = 0;  // cq: the query of the next step to take
   uint32_t dst = dst0, sdst = lds0 + 2 * kTile;
   const uint32_t dst_end = dst0 + NBUF * STAGE;
