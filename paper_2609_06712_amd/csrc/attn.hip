@@ -263,7 +263,7 @@ __global__ __launch_bounds__(256, QW == 4 ? 3 : 1) void attn_bf16_kernel(const F
 
 // fp32: four waves of 16 rows each walk the keys in tiles of 32 staged in LDS.
 template <int D>
-__global__ __launch_bounds__(256) void attn_f32x_kernel(const FwdArgs a) {
+__global__ __launch_bounds__(256, D == 64 ? 1 : 3) void attn_f32x_kernel(const FwdArgs a) {
   constexpr int W = D / 16, LD = D + 4, PT = 32 * D / 4 / 256;  // 16-byte pieces per thread, tensor and tile
   __shared__ __attribute__((aligned(16))) float ks[32 * LD], vs[32 * LD];
   const AttnCall& c = a.c;
@@ -349,7 +349,7 @@ __global__ __launch_bounds__(256) void attn_f32x_kernel(const FwdArgs a) {
 // fp32, few rows: a workgroup has 16 of them and its four waves take every fourth sub-tile of 16 keys, straight
 // from memory; they add up through LDS.
 template <int D>
-__global__ __launch_bounds__(256) void attn_f32_few_kernel(const FwdArgs a) {
+__global__ __launch_bounds__(256, D == 64 ? 1 : 2) void attn_f32_few_kernel(const FwdArgs a) {
   constexpr int W = D / 16;
   __shared__ __attribute__((aligned(16))) float os[4 * 16 * (D + 4)];
   __shared__ float2 mls[4][16];

@@ -118,8 +118,10 @@ inline Cut make_cut(int tiles, int bh, bool causal, int slots, int steps, double
   c.total = (int)(c.whole + left * c.splits);
   return c;
 }
-// fp32: tiles of 64 rows are so few that latency bounds them; 16-row tiles whose walk four waves share then.
-inline bool f32_few(long tiles, long bh) { return tiles * bh < 2 * kCus; }
+// fp32: tiles of 64 rows are so few that latency bounds them; 16-row tiles whose walk four waves share then. Below one
+// tile per CU: 2000 x 2000, one head, d 128 forward 43 us, with 64 rows 54; 384 tiles (2048 x 2048, 12 heads) 501 and
+// 341, dQ 561 and 562, dK/dV 666 and 656.
+inline bool f32_few(long tiles, long bh) { return tiles * bh < kCus; }
 inline long cut_left(const Cut& c) { return c.splits > 1 ? (c.total - c.whole) / c.splits : 0; }
 
 // Query head rows of one (b, key head): row r is query r / G of head hk G + r % G.

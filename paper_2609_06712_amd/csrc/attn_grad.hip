@@ -380,7 +380,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_bf16_kernel(const GradArgs a) 
 
 // fp32: four waves of 16 rows, key tiles of 32 staged in LDS.
 template <int D>
-__global__ __launch_bounds__(256) void attn_dq_f32_kernel(const GradArgs a) {
+__global__ __launch_bounds__(256, D == 64 ? 1 : 3) void attn_dq_f32_kernel(const GradArgs a) {
   constexpr int W = D / 16, LD = D + 4, PT = 32 * D / 4 / 256;
   __shared__ __attribute__((aligned(16))) float ks[32 * LD], vs[32 * LD];
   const AttnCall& c = a.c;
@@ -449,7 +449,7 @@ __global__ __launch_bounds__(256) void attn_dq_f32_kernel(const GradArgs a) {
 
 // fp32, few rows: 16 per workgroup, every fourth sub-tile of 16 keys per wave, straight from memory.
 template <int D>
-__global__ __launch_bounds__(256) void attn_dq_f32_few_kernel(const GradArgs a) {
+__global__ __launch_bounds__(256, D == 64 ? 1 : 2) void attn_dq_f32_few_kernel(const GradArgs a) {
   constexpr int W = D / 16;
   __shared__ __attribute__((aligned(16))) float os[4 * 16 * (D + 4)];
   const AttnCall& c = a.c;
@@ -764,7 +764,7 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_bf16_kernel(const GradArgs a)
 
 // fp32: four waves of 16 keys each, query tiles of 32 staged in LDS.
 template <int D>
-__global__ __launch_bounds__(256) void attn_dkv_f32_kernel(const GradArgs a) {
+__global__ __launch_bounds__(256, D == 64 ? 1 : 2) void attn_dkv_f32_kernel(const GradArgs a) {
   constexpr int W = D / 16, LD = D + 4, PT = 32 * D / 4 / 256;
   __shared__ __attribute__((aligned(16))) float qs[32 * LD], os[32 * LD];
   __shared__ float st[64];
@@ -851,7 +851,7 @@ __global__ __launch_bounds__(256) void attn_dkv_f32_kernel(const GradArgs a) {
 
 // fp32, few keys: 16 per workgroup, every fourth sub-tile of 16 queries per wave, straight from memory.
 template <int D>
-__global__ __launch_bounds__(256) void attn_dkv_f32_few_kernel(const GradArgs a) {
+__global__ __launch_bounds__(256, D == 64 ? 1 : 2) void attn_dkv_f32_few_kernel(const GradArgs a) {
   constexpr int W = D / 16;
   __shared__ __attribute__((aligned(16))) float os[4 * 16 * (D + 4)];
   const AttnCall& c = a.c;
