@@ -190,7 +190,7 @@ constexpr float kNoMax = -3e38f;
 //   f32_rows   X Y^T, X the tile, Y a row per lane in registers; step s of lane group g contracts channel
 //              g D/4 + s, so that both sides are read as 16-byte pieces;
 //   f32_cols   acc += X^T p, p[i] the value of tile row 4g + i (where f32_rows leaves it); row l%16 of channel
-//              tile w is channel (l%16) D/16 + w, again whole pieces.
+//              tile 4s + e is channel 64s + 4 (l%16) + e, again whole pieces, side by side over the lanes.
 template <int D>
 __device__ __forceinline__ f32x4 f32_rows(const float4 (&x)[D / 16], const float4 (&y)[D / 16]) {
   f32x4 s0 = f32x4{0.f, 0.f, 0.f, 0.f}, s1 = s0;
@@ -227,12 +227,12 @@ __device__ __forceinline__ f32x4 f32_rows(const float* tile, const float4 (&y)[D
 template <int D>
 __device__ __forceinline__ void f32_cols(const float* tile, const float (&p)[4], f32x4 (&acc)[D / 16],
                                          int lane) {
-  const float* at = tile + 4 * (lane / 16) * (D + 4) + (lane % 16) * (D / 16);
+  const float* at = tile + 4 * (lane / 16) * (D + 4) + (lane % 16) * 4;
   float4 x[4][D / 64];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int s = 0; s < D / 64; ++s) x[i][s] = *reinterpret_cast<const float4*>(at + i * (D + 4) + 4 * s);
+    for (int s = 0; s < D / 64; ++s) x[i][s] = *reinterpret_cast<const float4*>(at + i * (D + 4) + 64 * s);
   f32_cols<D>(x, p, acc);
 }
 // The second operand from memory: a lane's pieces of rows row0 + 4 g + i, those past `last` re-read that one.
@@ -243,7 +243,7 @@ __device__ __forceinline__ void f32_pieces(const char* base, long stride, int ro
   for (int i = 0; i < 4; ++i) {
     const char* row = base + min(row0 + 4 * (lane / 16) + i, last) * stride;
 #pragma unroll
-    for (int s = 0; s < D / 64; ++s) x[i][s] = reinterpret_cast<const float4*>(row)[(lane % 16) * (D / 64) + s];
+    for (int s = 0; s < D / 64; ++s) x[i][s] = reinterpret_cast<const float4*>(row)[lane % 16 + 16 * s];
   }
 }
 // A lane's quarter of a row, for f32_rows.
@@ -264,7 +264,7 @@ __device__ __forceinline__ void f32_join(float* lds, const f32x4 (&acc)[D / 16],
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int s = 0; s < W / 4; ++s)
-      *reinterpret_cast<float4*>(lds + (wave * 16 + lane % 16) * (D + 4) + (4 * (lane / 16) + i) * W + 4 * s) =
+      *reinterpret_cast<float4*>(lds + (wave * 16 + lane % 16) * (D + 4) + 64 * s + 4 * (4 * (lane / 16) + i)) =
           make_float4(acc[4 * s][i], acc[4 * s + 1][i], acc[4 * s + 2][i], acc[4 * s + 3][i]);
   __syncthreads();
 #pragma unroll
@@ -274,7 +274,7 @@ __device__ __forceinline__ void f32_join(float* lds, const f32x4 (&acc)[D / 16],
     for (int w = 0; w < 4; ++w) o[k] += lds[(w * 16 + threadIdx.x / 16) * (D + 4) + (threadIdx.x % 16) * W + k];
   }
 }
-// Stores a row from f32_cols' accumulators (lane: row l%16, channels (4g + i) W + w), scaled by f.
+// Stores a row from f32_cols' accumulators (lane: row l%16, channels 64 s + 4 (4g + i) + e), scaled by f.
 template <int D>
 __device__ __forceinline__ void f32_store(char* row, const f32x4 (&acc)[D / 16], float f, int lane) {
   constexpr int W = D / 16;
@@ -282,7 +282,7 @@ __device__ __forceinline__ void f32_store(char* row, const f32x4 (&acc)[D / 16],
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int s = 0; s < W / 4; ++s)
-      reinterpret_cast<float4*>(row)[((4 * (lane / 16) + i) * W) / 4 + s] =
+      reinterpret_cast<float4*>(row)[16 * s + 4 * (lane / 16) + i] =
           make_float4(acc[4 * s][i] * f, acc[4 * s + 1][i] * f, acc[4 * s + 2][i] * f, acc[4 * s + 3][i] * f);
 }
 
