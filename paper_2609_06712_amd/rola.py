@@ -991,7 +991,7 @@ def rola_norm(X, W=None, Bias=None, kind="layer", eps=1e-6, out=None, want_stats
     st = _stream_here(X, stream)
     mean = rstd = None
     if want_stats:
-        rstd = torch.empty(X.shape[:-1], dtype=torch.float32, device=X.device)
+        rstd = X.new_empty(X.shape[:-1], dtype=torch.float32)
         mean = torch.empty_like(rstd) if kind == "layer" else None
     prob = _norm_problem(*_norm_key(X, Bias if W is None else W, groups, kind))
     _check(LIB.rola_norm(prob, _ptr(X), ldx, _ptr(W), _ptr(Bias), eps, _ptr(out), ldy, _ptr(mean), _ptr(rstd),
@@ -1034,7 +1034,7 @@ def rola_norm_backward(X, W, mean, rstd, dY, kind="layer", want_bias=True, per_s
     st = _stream_here(X, stream)
     d = X.shape[-1]
     shape = (2, d) if groups == 1 else (2, groups, d)
-    both = torch.empty(shape, dtype=torch.float32, device=X.device)
+    both = X.new_empty(shape, dtype=torch.float32)
     if W is not None and W.dim() == 2 or (W is None and per_sample and X.dim() == 3):
         both = both.view(2, groups, d)
     dW, dB = both[0], both[1] if want_bias else None
