@@ -952,9 +952,16 @@ def _norm_params(a, x, w, name, dtype=None):
     return x.shape[0] if per_sample else 1
 
 
+def _fits(*sizes):
+    """The sizes of a problem, which has 32 bits for each; ctypes would take a larger one modulo 2^32."""
+    if max(sizes) >= 1 << 31:
+        raise ValueError(f"sizes must be below 2^31, got {sizes}")
+    return sizes
+
+
 @functools.lru_cache(maxsize=1024)
 def _norm_problem(rows, d, groups, kind, dtype, wdtype) -> NormProblem:
-    return NormProblem(rows, d, groups, kind, dtype, wdtype)
+    return NormProblem(*_fits(rows, d, groups), kind, dtype, wdtype)
 
 
 @functools.lru_cache(maxsize=1024)
@@ -1047,7 +1054,7 @@ def rola_norm_backward(X, W, mean, rstd, dY, kind="layer", want_bias=True, per_s
 
 @functools.lru_cache(maxsize=1024)
 def _attn_problem(B, H, Hkv, Nq, Nk, d, dtype, causal) -> AttnProblem:
-    return AttnProblem(B, H, Hkv, Nq, Nk, d, dtype, causal)
+    return AttnProblem(*_fits(B, H, Hkv, Nq, Nk, d), dtype, causal)
 
 
 @functools.lru_cache(maxsize=1024)

@@ -160,3 +160,16 @@ def test_binding_refuses_attn(change):
     args.update(change)
     with pytest.raises(ValueError):
         R.rola_attn(**args)
+
+
+def test_sizes_that_do_not_fit_the_problem_are_refused():
+    """A 32-bit field takes a larger size modulo 2^32: 2^32 + 8 rows would run as 8."""
+    x = torch.zeros(1, 8).expand(2 ** 32 + 8, 8)
+    q = torch.zeros(1, 1, 1, 128)
+    k = torch.zeros(1, 1, 1, 128).expand(1, 1, 2 ** 32 + 3, 128)
+    for call in (lambda: R._norm_problem(*R._norm_key(x, None, 1, "layer")),
+                 lambda: R.norm_backward_workspace_bytes(x), lambda: R.attn_workspace_bytes(q, k),
+                 lambda: R.attn_workspace_bytes(k, q, backward=True)):
+        with pytest.raises(ValueError, match="2\\^31"):
+            call()
+    assert R._norm_problem(2 ** 31 - 1, 8, 1, 0, 1, 0).rows == 2 ** 31 - 1
