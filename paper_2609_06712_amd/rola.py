@@ -1006,9 +1006,12 @@ def rola_norm(X, W=None, Bias=None, kind="layer", eps=1e-6, out=None, want_stats
     return out, mean, rstd
 
 
-def norm_backward_workspace_bytes(X, W=None, kind="layer") -> int:
-    return _norm_ws(*_norm_key(X, W, X.shape[0] if W is not None and W.dim() == 2 and X.dim() == 3 else 1,
-                               kind))
+def norm_backward_workspace_bytes(X, W=None, kind="layer", per_sample=None) -> int:
+    """Workspace of rola_norm_backward for these tensors; per_sample as there, without W."""
+    if kind not in NORM_KIND:
+        raise ValueError(f"kind must be one of {sorted(NORM_KIND)}, got {kind!r}")
+    per = per_sample if W is None else W.dim() == 2
+    return _norm_ws(*_norm_key(X, W, X.shape[0] if per and X.dim() == 3 else 1, kind))
 
 
 def rola_norm_backward(X, W, mean, rstd, dY, kind="layer", want_bias=True, per_sample=None, out=None, ws=None,

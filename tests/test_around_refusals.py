@@ -173,3 +173,12 @@ def test_sizes_that_do_not_fit_the_problem_are_refused():
         with pytest.raises(ValueError, match="2\\^31"):
             call()
     assert R._norm_problem(2 ** 31 - 1, 8, 1, 0, 1, 0).rows == 2 ** 31 - 1
+
+
+def test_workspace_of_gradients_per_sample_without_a_weight():
+    x, w = torch.zeros(7, 40, 64), torch.zeros(7, 64)
+    per = R.norm_backward_workspace_bytes(x, w)
+    assert per != R.norm_backward_workspace_bytes(x)
+    assert R.norm_backward_workspace_bytes(x, per_sample=True) == per
+    with pytest.raises(ValueError, match="kind"):
+        R.norm_backward_workspace_bytes(x, kind="batch")
