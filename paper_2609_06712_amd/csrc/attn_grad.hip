@@ -75,31 +75,34 @@ __global__ __launch_bounds__(256) void attn_stat_kernel(const GradArgs a, long r
   at[32] = none ? 0.f : s;
 }
 
+// A workgroup takes every gridDim.x-th set of 16 rows: one set each would be a grid of more than 2^32 threads from 2^28
+// rows on, which cannot be launched.
+constexpr int kRowdotGrid = 1 << 16;
 __global__ __launch_bounds__(256) void attn_rowdot_f32_kernel(int H, int Nq, int Np, int d, long rows, View O,
                                                               View dO, const float* __restrict__ lse,
                                                               float* __restrict__ stat) {
-  const long row = ((long)blockIdx.x * 256 + threadIdx.x) / 16;
   const int part = threadIdx.x % 16;
-  if (row >= rows) return;
-  const long bh = row / Np;
-  const int i = (int)(row % Np), b = (int)(bh / H), h = (int)(bh % H);
-  float s = 0.f;
-  if (i < Nq) {
-    const float4* x = reinterpret_cast<const float4*>(O.p + b * O.b + h * O.h + i * O.n);
-    const float4* y = reinterpret_cast<const float4*>(dO.p + b * dO.b + h * dO.h + i * dO.n);
-    for (int e = part; e < d / 4; e += 16) {
-      const float4 u = x[e], v = y[e];
-      s = fmaf(u.x, v.x, fmaf(u.y, v.y, fmaf(u.z, v.z, fmaf(u.w, v.w, s))));
+  for (long row = (long)blockIdx.x * 16 + threadIdx.x / 16; row < rows; row += (long)gridDim.x * 16) {
+    const long bh = row / Np;
+    const int i = (int)(row % Np), b = (int)(bh / H), h = (int)(bh % H);
+    float s = 0.f;
+    if (i < Nq) {
+      const float4* x = reinterpret_cast<const float4*>(O.p + b * O.b + h * O.h + i * O.n);
+      const float4* y = reinterpret_cast<const float4*>(dO.p + b * dO.b + h * dO.h + i * dO.n);
+      for (int e = part; e < d / 4; e += 16) {
+        const float4 u = x[e], v = y[e];
+        s = fmaf(u.x, v.x, fmaf(u.y, v.y, fmaf(u.z, v.z, fmaf(u.w, v.w, s))));
+      }
     }
-  }
 #pragma unroll
-  for (int off = 8; off >= 1; off >>= 1) s += __shfl_xor(s, off, 16);
-  if (part == 0) {
-    const float l = i < Nq ? lse[bh * Nq + i] : -__builtin_inff();
-    const bool none = l == -__builtin_inff();
-    float* at = stat + stat_at(bh, Np, i);
-    at[0] = none ? __builtin_inff() : l;
-    at[32] = none ? 0.f : s;
+    for (int off = 8; off >= 1; off >>= 1) s += __shfl_xor(s, off, 16);
+    if (part == 0) {
+      const float l = i < Nq ? lse[bh * Nq + i] : -__builtin_inff();
+      const bool none = l == -__builtin_inff();
+      float* at = stat + stat_at(bh, Np, i);
+      at[0] = none ? __builtin_inff() : l;
+      at[32] = none ? 0.f : s;
+    }
   }
 }
 
@@ -1027,7 +1030,7 @@ hipError_t launch_attn_backward(const AttnShape& s, const HeadView& Q, const Hea
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(attn_stat_kernel, dim3((unsigned)((rows + 255) / 256)), dim3(256), 0, st, a, rows, stat);
   } else {
-    hipLaunchKernelGGL(attn_rowdot_f32_kernel, dim3((unsigned)((rows * 16 + 255) / 256)), dim3(256), 0, st, s.H,
+    hipLaunchKernelGGL(attn_rowdot_f32_kernel, dim3((unsigned)std::min<long>((rows + 15) / 16, kRowdotGrid)), dim3(256), 0, st, s.H,
                        s.Nq, p.Np, s.d, rows, view_of(O, false), a.c.O, lse, stat);
   }
   e = hipGetLastError();

@@ -209,3 +209,14 @@ def test_rows_and_guard_zones_untouched():
         A.check(str(i), view, want[i], bound[i])
         view.fill_(7.0)
         assert bool((t == 7.0).all())
+
+
+def test_f32_gradients_of_more_rows_than_one_turn_of_the_row_products():
+    """2^20 + 37 queries over two keys: the last rows' products come from a second turn."""
+    N = 2 ** 20 + 37
+    q, k, v, do = _inputs(1, 1, 1, N, 2, 64, F32, seed=9)
+    o, lse = R.rola_attn(q, k, v)
+    dq = R.rola_attn_backward(q, k, v, o, lse, do, dQ=_nan_like(q))[0]
+    tail = slice(N - 101, N)
+    want, bound = A.attention(q[:, :, tail], k, v, None, False, 64 ** -0.5, do[:, :, tail])
+    A.check("dq", dq[:, :, tail], want[2], bound[2])
