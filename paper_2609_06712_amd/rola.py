@@ -908,6 +908,19 @@ def _stream_here(x, stream):
     return _stream(stream)
 
 
+def _on_its_stream(fn):
+    """With a stream given, the whole call runs as on that stream: what it allocates then belongs to the stream, whose
+    kernels use it. From the current stream's memory a workspace would be free for that stream's next
+    allocation when the call returns, with the kernels still at work on it."""
+    @functools.wraps(fn)
+    def call(*args, stream=None, **kw):
+        if stream is None:
+            return fn(*args, **kw)
+        with torch.cuda.stream(stream):
+            return fn(*args, stream=stream, **kw)
+    return call
+
+
 def _norm_rows(a, x, name, like=None):
     """Row stride of a [rows, d] or [B, N, d] tensor whose rows follow each other at one stride."""
     if not isinstance(x, torch.Tensor):
@@ -976,7 +989,8 @@ def _norm_key(x, w, groups, kind):
     return x.numel() // d, d, groups or 1, NORM_KIND[kind], _DTYPE_CODES[x.dtype], wt
 
 
-def rola_norm(X, W=None, Bias=None, kind="layer", eps=1e-6, out=None, want_stats=False, stream=None):
+@_on_its_stream
+def rola_norm(X, W=None, Bias=None, kind="layer", eps=1e-6, out=None, want_stats=False, *, stream=None):
     """Layer norm ("layer") or RMS norm ("rms") of X [rows, d] or [B, N, d] (rows at one stride) with
     W and Bias [d], or [B, d] for a weight per sample; either may be None. Returns (Y, mean, rstd): with
     want_stats the fp32 statistics per row that rola_norm_backward takes (mean None for "rms"), else None."""
@@ -1014,8 +1028,9 @@ def norm_backward_workspace_bytes(X, W=None, kind="layer", per_sample=None) -> i
     return _norm_ws(*_norm_key(X, W, X.shape[0] if per and X.dim() == 3 else 1, kind))
 
 
+@_on_its_stream
 def rola_norm_backward(X, W, mean, rstd, dY, kind="layer", want_bias=True, per_sample=None, out=None, ws=None,
-                       stream=None):
+                       *, stream=None):
     """(dX in X's type, dW, dB fp32 in W's shape; dB None without want_bias) of rola_norm, from the
     statistics it kept. Without W (None) dW is that of a weight of ones; per_sample then says whether it (and
     dB) is [B, d] instead of [d]."""
@@ -1148,8 +1163,9 @@ def attn_workspace_bytes(Q, K, causal=False, backward=False) -> int:
                     1 if causal else 0)
 
 
+@_on_its_stream
 def rola_attn(Q, K, V, kv_len=None, causal=False, scale=None, out=None, lse=None, want_lse=True, ws=None,
-              stream=None):
+              *, stream=None):
     """(O, lse): softmax attention of Q [B, H, Nq, d_h] over K, V [B, Hkv, Nk, d_h], H a multiple of
     Hkv. kv_len (int32 [B], on the device): keys per sample; causal: query i sees keys
     j <= i + kv_len - Nq. Tensors are taken in place by their strides (unit inner stride), so views of packed
@@ -1170,8 +1186,9 @@ def rola_attn(Q, K, V, kv_len=None, causal=False, scale=None, out=None, lse=None
     return out, lse
 
 
+@_on_its_stream
 def rola_attn_backward(Q, K, V, O, lse, dO, kv_len=None, causal=False, scale=None, dQ=None, dK=None, dV=None,
-                       ws=None, stream=None):
+                       ws=None, *, stream=None):
     """(dQ, dK, dV) of rola_attn in the inputs' type, from its O and lse; kv_len, causal and scale as in
     the forward. Outputs come in the order of heads and tokens of Q, K and V, or are the tensors given."""
     key, device, hq, hk, hv = _attn_args(Q, K, V, kv_len, causal)

@@ -220,3 +220,39 @@ def test_f32_gradients_of_more_rows_than_one_turn_of_the_row_products():
     tail = slice(N - 101, N)
     want, bound = A.attention(q[:, :, tail], k, v, None, False, 64 ** -0.5, do[:, :, tail])
     A.check("dq", dq[:, :, tail], want[2], bound[2])
+
+
+def test_workspace_of_another_stream_is_not_given_out_again(monkeypatch):
+    """After a call on a given stream, the current stream's next allocations are not the call's workspace."""
+    from paper_2609_06712_amd import rola
+
+    taken = []
+
+    class Calls:
+        def __getattr__(self, name):
+            fn = getattr(lib, name)
+
+            def call(*args):
+                if name in ("rola_attn", "rola_attn_backward"):
+                    taken.append((args[-3], args[-2]))
+                return fn(*args)
+            return call
+
+    lib = rola.LIB
+    q, k, v, do = _inputs(1, 2, 1, 20, 1500, 128, BF, seed=12)
+    want = R.rola_attn(q, k, v)
+    want += R.rola_attn_backward(q, k, v, *want, do)
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    monkeypatch.setattr(rola, "LIB", Calls())
+    st = torch.cuda.Stream()
+    got = R.rola_attn(q, k, v, stream=st)
+    got += R.rola_attn_backward(q, k, v, *got, do, stream=st)
+    again = [torch.empty(n, dtype=torch.uint8, device="cuda") for _, n in taken for _ in range(3)]
+    torch.cuda.synchronize()
+    assert len(taken) == 2 and all(n > 0 for _, n in taken)
+    for x in again:
+        for p, n in taken:
+            assert x.data_ptr() + x.numel() <= p or p + n <= x.data_ptr()
+    for x, y in zip(got, want):
+        assert torch.equal(x, y)
