@@ -7,12 +7,14 @@
 // bf16 (d 128), on v_mfma_f32_32x32x16_bf16, keys in sub-tiles of 32:
 //   S^T = K Q^T     A = K rows from LDS, B = Q in registers; a lane has one row and 16 keys of it;
 //   O^T = V^T P^T   A = V^T through the transposing LDS read, in the order the lane holds its keys.
-// P is rounded to bf16 for that product (relative 2^-9 of a term, as the inputs); the row sum adds the
+// P is rounded to bf16 for that product (half a step, at most 2^-8 of a term, as the inputs); the row sum adds the
 // probabilities before that rounding, so that lse is an fp32 value. O^T is rescaled only when a row's maximum
 // grows by more than 2^8, which leaves the quotient as it is.
 //   QW = 4: four waves of 32 rows each walk the keys together, three LDS stages, three workgroups per CU.
 //   QW = 1: few rows (R <= 32): the four waves take every fourth sub-tile of the same rows through stages of
 //           their own, without barriers, and add up through LDS.
+// Measured in a kernel trace: 8400 x 8400, 12 heads 392 us (1.11 PFLOP/s, matrix cores busy 0.77 of the cycles); one
+// token of 40 heads over 8 caches of 8 key heads, 32760 to 4679 keys, 135 us (613 MB: 4.5 TB/s) and 6 for the join.
 // The tiles of rows that do not fill a round of the chip are cut over their keys (Cut); the partial results (fp32,
 // with maximum and sum) are joined by attn_join_kernel in a fixed order.
 //

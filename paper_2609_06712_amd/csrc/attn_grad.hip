@@ -2,9 +2,11 @@
 //   P = exp2(S scale log2e - lse),  D = rowsum(dO O),  dP = dO V^T,  dS = P (dP - D),
 //   dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO  (dK, dV summed over the query heads of a key head).
 // The probabilities are recomputed, twice, so that every gradient is summed in registers in a fixed order
-// and is rounded once: a pass over the keys per tile of rows (dQ, three products) and a pass over the queries
-// per block of keys (dK, dV, four). Bound by the matrix cores (14 d operations per visible pair against the ten
-// of a single pass, which would have to add dQ in memory).
+// and is rounded once: a pass over the keys per tile of rows (dQ, three products; four in bf16, whose dS is two
+// terms) and a pass over the queries per block of keys (dK, dV, four). Bound by the matrix cores: 14 d operations
+// per visible pair (bf16, with the pass for D: 20 d) against the ten of a single pass, which would have to add dQ in
+// memory. Measured in a kernel trace, bf16, 8400 x 8400, 12 heads: D 355 us (1.22 PFLOP/s), dQ 761 (1.14), dK and dV
+// 909 (0.95); matrix cores busy 0.77, 0.69 and 0.52 of the cycles.
 //
 // D. It is rowsum(dO O), but from an O that was rounded to bf16 it is off by dO times that rounding, for all
 // keys of a row alike: sum_j P_ij K_j times the error reaches dQ, where sum_j dS_ij K_j has cancelled (8400 keys:

