@@ -118,9 +118,16 @@ inline Cut make_cut(int tiles, int bh, bool causal, int slots, int steps, double
   c.total = (int)(c.whole + left * c.splits);
   return c;
 }
-// fp32: tiles of 64 rows are so few that latency bounds them; 16-row tiles whose walk four waves share then. Below one
-// tile per CU: 2000 x 2000, one head, d 128 forward 43 us, with 64 rows 54; 384 tiles (2048 x 2048, 12 heads) 501 and
-// 341, dQ 561 and 562, dK/dV 666 and 656.
+// fp32: 16-row tiles whose walk four waves share, where tiles of 64 rows are so few that latency bounds them: below one
+// tile per CU (2048 x 2048, 12 heads, 384 tiles, d 128: forward 501 us with 16 rows, 341 with 64), and below an amount of
+// work B H Nq Nk d, as every 16 rows read the walk again from memory. Calls in us with 16 rows and with 64:
+//   forward, d 128: 12 x 500 x 1100 (0.8e9) 80 and 86; 2700 x 2700 (0.9e9) 91 and 80; 2 x 4000 x 4000 (4e9) 298 and
+//   220. At d 64 a tile's walk is half as long in bytes and 16 rows are the faster up to the 2e9 that was tried
+//   (2 x 4000 x 4000: 115 and 127).
+//   gradients: 4 x 3000 x 300, d 128 (0.5e9) 126 and 145; 3 x 2000 x 1000, d 128 (0.8e9) 206 and 182; 2 x 4000 x 4000,
+//   d 64 (2e9) 373 and 330. Not in order at d 64: 6 x 1500 x 1000 (0.6e9) 148 and 139, 8 x 600 x 6000 (1.8e9) 305 and 320.
+constexpr double kFewForward = 0.9e9, kFewGrad = 0.55e9;
+inline double attn_work(const AttnShape& s) { return (double)s.B * s.H * s.Nq * s.Nk * s.d; }
 inline bool f32_few(long tiles, long bh) { return tiles * bh < kCus; }
 inline long cut_left(const Cut& c) { return c.splits > 1 ? (c.total - c.whole) / c.splits : 0; }
 

@@ -969,8 +969,9 @@ GradPlan grad_plan(const AttnShape& s) {
   if (s.bf16) {
     p.rows = p.keys = 128;
   } else {
-    p.rows = f32_few((p.R + 63) / 64, bh) ? 16 : 64;
-    p.keys = f32_few((s.Nk + 63) / 64, bh) ? 16 : 64;
+    const bool little = attn_work(s) < kFewGrad;
+    p.rows = little && f32_few((p.R + 63) / 64, bh) ? 16 : 64;
+    p.keys = little && f32_few((s.Nk + 63) / 64, bh) ? 16 : 64;
   }
   const int qtiles = (p.R + p.rows - 1) / p.rows, ktiles = (s.Nk + p.keys - 1) / p.keys;
   const double qbytes = p.rows * s.d * 4.0, kbytes = p.keys * s.d * 4.0;

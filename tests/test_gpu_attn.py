@@ -256,3 +256,14 @@ def test_workspace_of_another_stream_is_not_given_out_again(monkeypatch):
             assert x.data_ptr() + x.numel() <= p or p + n <= x.data_ptr()
     for x, y in zip(got, want):
         assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("B,H,Hkv,Nq,Nk,d,lens,causal", [
+    (1, 3, 3, 700, 2900, 128, None, False),      # 64-row tiles, cut: forward and gradients
+    (2, 4, 2, 309, 3100, 128, [3100, 1777], False),
+    (1, 4, 2, 1201, 1190, 128, None, True),      # 64-row tiles in the gradients only
+    (1, 4, 4, 1500, 1600, 64, [1533], False),    # d 64: 16-row tiles forward, 64 in the gradients
+    (1, 2, 1, 1100, 1500, 128, [1100], True),    # 16-row tiles in both
+])
+def test_f32_tiles_by_the_amount_of_work(B, H, Hkv, Nq, Nk, d, lens, causal):
+    _run(B, H, Hkv, Nq, Nk, lens, causal, F32, d, packed=True, seed=13)
