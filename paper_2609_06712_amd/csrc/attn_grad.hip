@@ -13,8 +13,9 @@
 // dQ off by 0.0048 of its norm, where its own rounding is 0.0017). So bf16 sums it in fp32 from what the
 // gradients use, D = rowsum(P dP), in a pass of two products (attn_rowsum_bf16_kernel); fp32 takes dO O.
 //
-// Row statistics: per query lse and D, in tiles of 32 queries [32 lse][32 D], per head padded to whole tiles with
-// lse = inf: P is then zero for rows past the last and for rows that see no key, with no test in the walk.
+// Row statistics: per query lse (bf16: less kLift) and D, in tiles of 32 queries [32 lse][32 D], per head padded to
+// whole tiles with lse = inf: P is then zero for rows past the last and for rows that see no key, with no test in the
+// walk.
 //
 // The tiles that do not fill a round of the chip are cut (Cut); the parts' fp32 sums go to the workspace and are
 // added in order by attn_sum_kernel.
@@ -27,6 +28,13 @@ namespace {
 
 constexpr int kRows = 32;            // rows of a sub-tile
 constexpr int kTile = kRows * 256;   // its bytes (bf16, d 128)
+// The bf16 dK/dV pass works with 2^15 P: one role hands it to the other as fp16, whose normal range starts at 2^-14, and
+// many keys, or one that takes nearly all of a row, leave the others less. Lifted, P fills that range up to its end (32768
+// of 65504) and is rounded by half a step of fp16 from 2^-29 on. Without it P below 2^-25 gave dK = 0, dK of 300000
+// keys was off by 0.0039 of its norm (0.0024), and single keys beside one that takes 0.999 of 8400 by up to 0.064 of
+// theirs (0.0049). The factor is a power of two, so no other rounding changes but that of lse - 15, 2^-21 at most below
+// an lse of 31. The times do not change.
+constexpr float kLift = 15.f, kDrop = 1.f / 32768;
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -53,7 +61,7 @@ struct GradArgs {
 // Where the statistics of query i of a head are: lse there, D 32 further.
 __device__ __forceinline__ long stat_at(long head, int Np, int i) { return (head * (Np / 32) + i / 32) * 64 + i % 32; }
 
-// lse and D (of a cut tile the sum of its parts) into tiles; queries as rows i G + g of their key head.
+// lse, less kLift, and D (of a cut tile the sum of its parts) into tiles; queries as rows i G + g of their key head.
 __global__ __launch_bounds__(256) void attn_stat_kernel(const GradArgs a, long rows, float* __restrict__ stat) {
   const long row = (long)blockIdx.x * 256 + threadIdx.x;  // (b, h, padded query)
   if (row >= rows) return;
@@ -73,7 +81,7 @@ __global__ __launch_bounds__(256) void attn_stat_kernel(const GradArgs a, long r
   }
   const bool none = l == -__builtin_inff();
   float* at = stat + stat_at(head, a.Np, i);
-  at[0] = none ? __builtin_inff() : l;
+  at[0] = none ? __builtin_inff() : l - kLift;
   at[32] = none ? 0.f : s;
 }
 
@@ -275,8 +283,9 @@ __global__ __launch_bounds__(256, 2) void attn_dq_bf16_kernel(const GradArgs a) 
       df[s] = *reinterpret_cast<const bf16x8*>(o + 32 * s);
     }
   }
-  const float* st = a.stat + stat_at((long)pt.b * a.H + head, a.Np, i);
-  const float lse = st[0], dsum = st[32];
+  float lse = a.lse[((long)pt.b * a.H + head) * c.Nq + i];
+  if (lse == -__builtin_inff()) lse = __builtin_inff();
+  const float dsum = a.stat[stat_at((long)pt.b * a.H + head, a.Np, i) + 32];
   wait_vm<0>();
   f32x16 acc[4];
 #pragma unroll
@@ -524,8 +533,8 @@ __device__ __forceinline__ Walk walk_of(const GradArgs& a, int n, int key0, cons
 
 // bf16: a workgroup has 128 keys, in two roles of two waves over the same 64-key columns. Role 0 holds the
 // keys' K: S = Q K^T, P, dV^T += dO^T P. Role 1 holds their V: dP = dO V^T, dS = P (dP - D), dK^T += Q^T dS, with
-// P from role 0 through LDS one step later, as fp16 (P lies in [0, 1], where that is an eighth of the
-// rounding to bf16 that dS takes next). A wave has its SIMD to itself: two 32-key tiles, so that what it reads
+// P from role 0 through LDS one step later, as fp16 (an eighth of the rounding to bf16 that dS takes next). Both
+// gradients carry P's factor 2^15 (kLift) to the end. A wave has its SIMD to itself: two 32-key tiles, so that what it reads
 // from LDS serves two products (one tile per wave and two waves per SIMD read 1.5 times what the LDS delivers
 // while the products run), and the softmax of one tile lies between the products of the other:
 //   S_0 | S_1 with P_0 | dV_0 with P_1 and the next step's row operand | dV_1.
@@ -656,10 +665,10 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_bf16_kernel(const GradArgs a)
       const char* tile = stage + (1 - ROLE) * kTile;                          // read transposed
       const char* next = lds + (ROLE ? buf : ahead) * STAGE + ROLE * kTile;  // the next step's rows
       bf16x8 fb[8];
-      float lv[16];  // lse (role 0) or D (role 1) of the step's queries 8 (k / 4) + 4 hh + k % 4
+      float lv[16];  // lse less kLift (role 0) or D (role 1) of the step's queries 8 (k / 4) + 4 hh + k % 4
       uint32_t ph[2][8], b2[2][8];  // pairs of fp16 P; of bf16 P or dS
       f32x16 X[2] = {f32x16{}, f32x16{}};
-      // P or dS of the queries k, k + 1 of tile u. (The empty assembly keeps the work where it stands: the compiler
+      // P or dS (2^15 of either) of the queries k, k + 1 of tile u. (The empty assembly keeps the work where it stands: the compiler
       // would otherwise sink it past the products it is to lie between.)
       auto middle = [&](int u, int k) {
         if constexpr (ROLE == 0) {
@@ -754,7 +763,7 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_bf16_kernel(const GradArgs a)
 #pragma unroll
       for (int w = 0; w < 4; ++w) acc[u][w] = f32x16{};
     }
-    const float f = role ? c.scale : 1.f;
+    const float f = role ? c.scale * kDrop : kDrop;
     if (pt.left >= 0) {
       if (k >= c.Nk) break;
       float* out = a.part + (role ? 0 : a.part2) + (((long)pt.left * pt.splits + pt.split) * 128 + k - key0) * 128;

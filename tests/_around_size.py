@@ -8,12 +8,12 @@ What is rounded: every result once; P for O and dV; dS for dK, from a P that is 
 half of that type's least step over 2^15; dS in two terms (U^2) for dQ.
 
 D is an fp32 sum over a row's n keys, and its error d_i is the same for all of them, so dQ_i is off by
-d_i scale |sum_j P_ij K_j|. In units of 2^-24 of sum_j P |dP|, which no partial sum exceeds: a lane adds half a row's
+d_i scale |sum_j P_ij K_j|, and dK_j by the d_i scale P_ij |Q_i| of independent rows. In units of 2^-24 of sum_j P |dP|, which no partial sum exceeds: a lane adds half a row's
 terms one after the other, n / 2 roundings of at most one unit each; the probabilities' sum adds eight at a time,
 n / 16; the log-sum-exp is rounded at |lse| 2^-24, ln 2 times that in P; the scores, exp2 and the last sums 16. That
 is the bound for one row (where one key holds most of it, each of the others may round the same way: an emulation
 of the sum in fp32 is off by up to 654 units at 8400 keys, the bound being about 4760). Over all rows the roundings are
-independent: sqrt(n / 2) for the sum, the others as before.
+independent: sqrt(n / 2) and sqrt(n / 16) for the sums, the others as before.
 """
 
 import math
@@ -35,7 +35,7 @@ def reference(q, k, v, lens, causal, scale, do):
     q, k, v, do = (t.to(F64) for t in (q, k, v, do))
     val = dict(o=torch.zeros_like(q), dq=torch.zeros_like(q), dk=torch.zeros_like(k), dv=torch.zeros_like(k))
     err = {n: torch.zeros(x.shape[:-1], dtype=F64, device=q.device) for n, x in val.items()}
-    worst, usual = torch.zeros_like(err["dq"]), torch.zeros_like(err["dq"])
+    worst, usual = ({n: torch.zeros_like(x) for n, x in err.items()} for _ in range(2))
     sq = lambda x: x.square().sum(-1)
     for b in range(B):
         n = Nk if lens is None else lens[b]
@@ -52,16 +52,18 @@ def reference(q, k, v, lens, causal, scale, do):
             val["o"][b, h], err["o"][b, h] = p @ V, p.square() @ sq(V)
             val["dq"][b, h] = ds @ K
             err["dq"][b, h] = (U * ds).square() @ sq(K)
-            unit = E32 / U * scale * (p * dp.abs()).sum(-1) * sq(p @ K).sqrt()
-            rest = torch.logsumexp(s, -1).abs() + n / 16 + 16
-            worst[b, h], usual[b, h] = ((n / 2 + rest) * unit).square(), ((n / 2) ** 0.5 * unit).square()
-            usual[b, h] += (rest * unit).square()
+            unit = E32 / U * scale * (p * dp.abs()).sum(-1)
+            rest, sums = torch.logsumexp(s, -1).abs() + 16, n / 2 + n / 16
+            for to, units in ((worst, (sums + rest).square()), (usual, sums + rest.square())):
+                d2 = units * unit.square()
+                to["dq"][b, h] = d2 * sq(p @ K)
+                to["dk"][b, g, :n] += p.square().t() @ (d2 * sq(Q))
             val["dk"][b, g, :n] += ds.t() @ Q
             low = 2.0 ** -40 * scale * (dp - D)
             err["dk"][b, g, :n] += ((1 + U16 / U) * ds).square().t() @ sq(Q) + (low / U).square().t() @ sq(Q)
             val["dv"][b, g, :n] += p.t() @ dO
             err["dv"][b, g, :n] += p.square().t() @ sq(dO)
-    return {name: (val[name], err[name], *((worst, usual) if name == "dq" else (0.0, 0.0))) for name in val}
+    return {name: (val[name], err[name], worst[name], usual[name]) for name in val}
 
 
 def excess(got, ref):
