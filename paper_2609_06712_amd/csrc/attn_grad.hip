@@ -849,7 +849,10 @@ __global__ __launch_bounds__(256, D == 64 ? 1 : 2) void attn_dkv_f32_kernel(cons
     }
   }
   if (key >= c.Nk) return;
-  const float live = key < n ? 1.f : 0.f;
+  if (key >= n) {  // a key that is not there (its lane walked with the last one's row)
+#pragma unroll
+    for (int w = 0; w < W; ++w) dk[w] = dv[w] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
   char *pk, *pv;
   if (pt.left >= 0) {
     float* out = a.part + (((long)pt.left * pt.splits + pt.split) * 64 + key - key0) * D;
@@ -859,8 +862,8 @@ __global__ __launch_bounds__(256, D == 64 ? 1 : 2) void attn_dkv_f32_kernel(cons
     pk = a.G1.p + pt.b * a.G1.b + pt.hk * a.G1.h + key * a.G1.n;
     pv = a.G2.p + pt.b * a.G2.b + pt.hk * a.G2.h + key * a.G2.n;
   }
-  f32_store<D>(pk, dk, c.scale * live, lane);
-  f32_store<D>(pv, dv, live, lane);
+  f32_store<D>(pk, dk, c.scale, lane);
+  f32_store<D>(pv, dv, 1.f, lane);
 }
 
 // fp32, few keys: 16 per workgroup, every fourth sub-tile of 16 queries per wave, straight from memory.
@@ -913,7 +916,11 @@ __global__ __launch_bounds__(256, D == 64 ? 1 : 2) void attn_dkv_f32_few_kernel(
   f32_join<D>(os, dv, wave, lane, ov);
   const int k = key0 + threadIdx.x / 16, c0 = (threadIdx.x % 16) * W;
   if (k >= c.Nk) return;
-  const float live = k < n ? 1.f : 0.f, f = c.scale * live;
+  if (k >= n) {  // a key that is not there (its lane walked with the last one's row)
+#pragma unroll
+    for (int w = 0; w < W; ++w) ok[w] = ov[w] = 0.f;
+  }
+  const float f = c.scale;
   float *pk, *pv;
   if (pt.left >= 0) {
     pk = a.part + (((long)pt.left * pt.splits + pt.split) * 16 + k - key0) * D;
@@ -927,7 +934,7 @@ __global__ __launch_bounds__(256, D == 64 ? 1 : 2) void attn_dkv_f32_few_kernel(
     reinterpret_cast<float4*>(pk + c0)[s] =
         make_float4(ok[4 * s] * f, ok[4 * s + 1] * f, ok[4 * s + 2] * f, ok[4 * s + 3] * f);
     reinterpret_cast<float4*>(pv + c0)[s] =
-        make_float4(ov[4 * s] * live, ov[4 * s + 1] * live, ov[4 * s + 2] * live, ov[4 * s + 3] * live);
+        make_float4(ov[4 * s], ov[4 * s + 1], ov[4 * s + 2], ov[4 * s + 3]);
   }
 }
 
