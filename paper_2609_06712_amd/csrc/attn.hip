@@ -238,14 +238,14 @@ __global__ __launch_bounds__(256, QW == 4 ? 3 : 1) void attn_bf16_kernel(const F
       return;
     }
     const int ii = rr / c.G, gg = rr % c.G, head = pt.hk * c.G + gg;
-    const float f = sum > 0.f ? 1.f / sum : 0.f;
+    const float f = row_inverse(sum);
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[e] *= f;
     bf16* out = reinterpret_cast<bf16*>(c.O.p + pt.b * c.O.b + head * c.O.h + ii * c.O.n) + c0;
     store8(out, o);
     store8(out + 8, o + 8);
     if (a.lse && c0 == 0)
-      a.lse[(pt.b * a.heads + head) * c.Nq + ii] = sum > 0.f ? mx + __log2f(sum) : -__builtin_inff();
+      a.lse[(pt.b * a.heads + head) * c.Nq + ii] = row_lse(mx, sum);
   } else {
     if (pt.left >= 0) {
       const long at = ((long)pt.left * pt.splits + pt.split) * 128 + wave * 32 + lane % 32;
@@ -255,11 +255,11 @@ __global__ __launch_bounds__(256, QW == 4 ? 3 : 1) void attn_bf16_kernel(const F
       return;
     }
     __syncthreads();  // every wave is done with the stages
-    rows_from_acc(lds + wave * 8192, acc, l > 0.f ? 1.f / l : 0.f, row_base(c.O, pt.b, pt.hk, c.G), row0, a.R, lane);
+    rows_from_acc(lds + wave * 8192, acc, row_inverse(l), row_base(c.O, pt.b, pt.hk, c.G), row0, a.R, lane);
     int q = row0 + lane % 32;
     asm volatile("" : "+v"(q));  // (divided again here, or the first quotient stays in a register all the way)
     if (a.lse && hh == 0 && q < a.R)
-      a.lse[(pt.b * a.heads + pt.hk * c.G + q % c.G) * c.Nq + q / c.G] = l > 0.f ? m + __log2f(l) : -__builtin_inff();
+      a.lse[(pt.b * a.heads + pt.hk * c.G + q % c.G) * c.Nq + q / c.G] = row_lse(m, l);
   }
 }
 
@@ -343,9 +343,9 @@ __global__ __launch_bounds__(256, D == 64 ? 1 : 3) void attn_f32x_kernel(const F
     return;
   }
   const int head = pt.hk * c.G + g;
-  f32_store<D>(c.O.p + pt.b * c.O.b + head * c.O.h + i * c.O.n, acc, l > 0.f ? 1.f / l : 0.f, lane);
+  f32_store<D>(c.O.p + pt.b * c.O.b + head * c.O.h + i * c.O.n, acc, row_inverse(l), lane);
   if (a.lse && gr == 0)
-    a.lse[(pt.b * a.heads + head) * c.Nq + i] = l > 0.f ? m + __log2f(l) : -__builtin_inff();
+    a.lse[(pt.b * a.heads + head) * c.Nq + i] = row_lse(m, l);
 }
 
 // fp32, few rows: a workgroup has 16 of them and its four waves take every fourth sub-tile of 16 keys, straight
@@ -421,7 +421,7 @@ __global__ __launch_bounds__(256, D == 64 ? 1 : 2) void attn_f32_few_kernel(cons
   for (int w = 0; w < 4; ++w) sum = fmaf(__builtin_amdgcn_exp2f(mls[w][row].x - mx), mls[w][row].y, sum);
   const int ii = rr / c.G, head = pt.hk * c.G + rr % c.G;
   const long at = ((long)pt.left * pt.splits + pt.split) * 16 + row;
-  const float inv = pt.left >= 0 ? 1.f : sum > 0.f ? 1.f / sum : 0.f;
+  const float inv = pt.left >= 0 ? 1.f : row_inverse(sum);
   float* out = pt.left >= 0 ? a.part + at * D
                             : reinterpret_cast<float*>(c.O.p + pt.b * c.O.b + head * c.O.h + ii * c.O.n);
 #pragma unroll
@@ -432,7 +432,7 @@ __global__ __launch_bounds__(256, D == 64 ? 1 : 2) void attn_f32_few_kernel(cons
   if (pt.left >= 0)
     a.ml[at] = make_float2(mx, sum);
   else if (a.lse)
-    a.lse[(pt.b * a.heads + head) * c.Nq + ii] = sum > 0.f ? mx + __log2f(sum) : -__builtin_inff();
+    a.lse[(pt.b * a.heads + head) * c.Nq + ii] = row_lse(mx, sum);
 }
 
 // Joins the parts of a cut tile's rows: a wave per row, D / 64 channels per lane.
@@ -474,12 +474,12 @@ __global__ __launch_bounds__(256) void attn_join_kernel(const FwdArgs a) {
     }
   }
   const int b = (int)(bh / c.Hkv), i = r / c.G, head = (int)(bh % c.Hkv) * c.G + r % c.G;
-  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  const float inv = row_inverse(sum);
   T* out = reinterpret_cast<T*>(c.O.p + b * c.O.b + head * c.O.h + i * c.O.n) + lane * V;
 #pragma unroll
   for (int k = 0; k < V; ++k) out[k] = from_f32<T>(o[k] * inv);
   if (a.lse && lane == 0)
-    a.lse[(b * a.heads + head) * c.Nq + i] = sum > 0.f ? mx + __log2f(sum) : -__builtin_inff();
+    a.lse[(b * a.heads + head) * c.Nq + i] = row_lse(mx, sum);
 }
 
 // How a call is cut: rows per tile, and the parts of the tiles.

@@ -190,6 +190,14 @@ __device__ __forceinline__ float halves_max(float x) {
 // Reference max of a row that has seen no key yet: below every finite score, and finite, so that a hidden
 // key's exp2(-inf - m) is zero and not NaN.
 constexpr float kNoMax = -3e38f;
+// 1 / l and log2 of a row's denominator, from its maximum m and sum l; of a row that has seen no key (l is the zero it
+// started from) 0 and -inf, the mark by which the gradients leave it out. A NaN or +inf score makes l NaN, and
+// both results. (By its bits: the library is built with NaN compares free to go either way.)
+__device__ __forceinline__ float row_inverse(float l) { return __float_as_uint(l) == 0 ? 0.f : 1.f / l; }
+__device__ __forceinline__ float row_lse(float m, float l) {
+  return __float_as_uint(l) == 0 ? -__builtin_inff() : m + __log2f(l);
+}
+__device__ __forceinline__ bool saw_no_key(float lse) { return __float_as_uint(lse) == 0xff800000u; }  // -inf
 
 // ---- fp32 tiles -------------------------------------------------------------------------------------
 // On v_mfma_f32_16x16x4_f32 (A: row l%16, k = l/16; B: column l%16, k = l/16; D: column l%16, rows

@@ -79,7 +79,7 @@ __global__ __launch_bounds__(256) void attn_stat_kernel(const GradArgs a, long r
       for (int k = 0; k < S; ++k) s += p[k * 256];
     }
   }
-  const bool none = l == -__builtin_inff();
+  const bool none = saw_no_key(l);
   float* at = stat + stat_at(head, a.Np, i);
   at[0] = none ? __builtin_inff() : l - kLift;
   at[32] = none ? 0.f : s;
@@ -108,7 +108,7 @@ __global__ __launch_bounds__(256) void attn_rowdot_f32_kernel(int H, int Nq, int
     for (int off = 8; off >= 1; off >>= 1) s += __shfl_xor(s, off, 16);
     if (part == 0) {
       const float l = i < Nq ? lse[bh * Nq + i] : -__builtin_inff();
-      const bool none = l == -__builtin_inff();
+      const bool none = saw_no_key(l);
       float* at = stat + stat_at(bh, Np, i);
       at[0] = none ? __builtin_inff() : l;
       at[32] = none ? 0.f : s;
@@ -160,7 +160,7 @@ __global__ __launch_bounds__(256, 2) void attn_rowsum_bf16_kernel(const GradArgs
       df[u][s] = *reinterpret_cast<const bf16x8*>(o + 32 * s);
     }
     lse[u] = a.lse[((long)pt.b * a.H + head) * c.Nq + i];
-    if (lse[u] == -__builtin_inff()) lse[u] = __builtin_inff();
+    if (saw_no_key(lse[u])) lse[u] = __builtin_inff();
   }
   wait_vm<0>();
 
@@ -284,7 +284,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_bf16_kernel(const GradArgs a) 
     }
   }
   float lse = a.lse[((long)pt.b * a.H + head) * c.Nq + i];
-  if (lse == -__builtin_inff()) lse = __builtin_inff();
+  if (saw_no_key(lse)) lse = __builtin_inff();
   const float dsum = a.stat[stat_at((long)pt.b * a.H + head, a.Np, i) + 32];
   wait_vm<0>();
   f32x16 acc[4];
