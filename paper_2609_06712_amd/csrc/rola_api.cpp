@@ -243,29 +243,24 @@ bool self_disjoint(const Rows& v) {
   return true;
 }
 
-// Whether two tensors may share bytes: their ranges meet, and they are not parts of one packed tensor whose
-// pieces (of a token, or of a sample) lie side by side within the same stride.
+// Whether two tensors may share bytes: their ranges meet, and no stride s tells them apart. Modulo s, a dimension that
+// steps by multiples of s stands still, and the others span a window from the first element on; two tensors whose
+// windows do not meet there share no byte, whatever their sizes. So the parts of one packed tensor pass, in any order
+// of its dimensions: s is the stride of the dimension that the parts lie within.
 bool rows_overlap(const Rows& a, const Rows& b) {
   if (!overlap(a.p, (size_t)a.end(), b.p, (size_t)b.end())) return false;
-  for (int level : {2, 0}) {  // the token stride, the sample stride
-    const long long s = a.stride[level];
-    if (s <= 0 || s != b.stride[level]) continue;
-    // everything but the dimensions that step by multiples of s lies within one window of s
-    long long wa = a.row, wb = b.row;
-    bool ok = true;
-    for (int i = 0; i < 3; ++i) {
-      if (i == level) continue;
-      const bool whole_a = a.size[i] == 1 || a.stride[i] % s == 0;
-      const bool whole_b = b.size[i] == 1 || b.stride[i] % s == 0;
-      if (whole_a && whole_b && level == 2 && i == 0) continue;  // whole samples of tokens
-      wa += (a.size[i] - 1) * a.stride[i];
-      wb += (b.size[i] - 1) * b.stride[i];
+  for (const Rows* t : {&a, &b})
+    for (const long long s : t->stride) {
+      if (s <= 0) continue;
+      long long wa = a.row, wb = b.row;
+      for (int i = 0; i < 3; ++i) {
+        if (a.stride[i] % s != 0) wa += (a.size[i] - 1) * a.stride[i];
+        if (b.stride[i] % s != 0) wb += (b.size[i] - 1) * b.stride[i];
+      }
+      if (wa > s || wb > s) continue;
+      const long long off = (((a.p - b.p) % s) + s) % s;  // a's window in b's frame
+      if (off >= wb && off + wa <= s) return false;
     }
-    ok = wa <= s && wb <= s;
-    if (!ok) continue;
-    const long long off = (((a.p - b.p) % s) + s) % s;  // a's window in b's frame
-    if (off >= wb && off + wa <= s) return false;
-  }
   return true;
 }
 
