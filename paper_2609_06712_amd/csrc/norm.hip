@@ -320,37 +320,36 @@ int norm_row_threads(long rows, int d, bool bwd) {
   return rows < kCus ? 256 : 64;
 }
 
-template <typename T, bool BWD, int TPR>
-void launch_norm_p(const NormArgs& a, dim3 grid, hipStream_t st) {
-  const int p = (a.d / 8 + TPR - 1) / TPR;
-  const auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(norm_threads<TPR>()), 0, st, a);
-  };
-  if constexpr (BWD) {
-    if (p == 1) go(norm_bwd_kernel<T, TPR, 1>);
-    else if (p == 2) go(norm_bwd_kernel<T, TPR, 2>);
-    else if (p == 3) go(norm_bwd_kernel<T, TPR, 3>);
-    else go(norm_bwd_kernel<T, TPR, 4>);
-  } else {
-    if (p == 1) go(norm_fwd_kernel<T, TPR, 1>);
-    else if (p == 2) go(norm_fwd_kernel<T, TPR, 2>);
-    else if (p == 3) go(norm_fwd_kernel<T, TPR, 3>);
-    else go(norm_fwd_kernel<T, TPR, 4>);
+// Pieces per thread that rows of d channels come to with the threads that norm_row_threads gives them: what there are
+// kernels for. 256 threads take up to 2048 channels (few rows) in either direction and the forward's up to 8192, 512
+// the backward's from there on and the forward's beyond 8192.
+template <bool BWD, int TPR>
+constexpr int kLeastPieces = TPR == 512 && !BWD ? 3 : 1;
+template <bool BWD, int TPR>
+constexpr int kMostPieces = TPR == 256 && BWD ? 1 : 4;
+
+template <typename T, bool BWD, int TPR, int P = kLeastPieces<BWD, TPR>>
+hipError_t launch_norm_p(const NormArgs& a, dim3 grid, hipStream_t st) {
+  if ((a.d / 8 + TPR - 1) / TPR == P) {
+    if constexpr (BWD)
+      hipLaunchKernelGGL((norm_bwd_kernel<T, TPR, P>), grid, dim3(norm_threads<TPR>()), 0, st, a);
+    else
+      hipLaunchKernelGGL((norm_fwd_kernel<T, TPR, P>), grid, dim3(norm_threads<TPR>()), 0, st, a);
+    return hipGetLastError();
   }
+  if constexpr (P < kMostPieces<BWD, TPR>) return launch_norm_p<T, BWD, TPR, P + 1>(a, grid, st);
+  return hipErrorInvalidConfiguration;
 }
 
 template <bool BWD>
 hipError_t launch_norm_t(bool bf, const NormArgs& a, int tpr, dim3 grid, hipStream_t st) {
-  if (bf) {
-    if (tpr == 64) launch_norm_p<bf16, BWD, 64>(a, grid, st);
-    else if (tpr == 256) launch_norm_p<bf16, BWD, 256>(a, grid, st);
-    else launch_norm_p<bf16, BWD, 512>(a, grid, st);
-  } else {
-    if (tpr == 64) launch_norm_p<float, BWD, 64>(a, grid, st);
-    else if (tpr == 256) launch_norm_p<float, BWD, 256>(a, grid, st);
-    else launch_norm_p<float, BWD, 512>(a, grid, st);
-  }
-  return hipGetLastError();
+  if (bf)
+    return tpr == 64    ? launch_norm_p<bf16, BWD, 64>(a, grid, st)
+           : tpr == 256 ? launch_norm_p<bf16, BWD, 256>(a, grid, st)
+                        : launch_norm_p<bf16, BWD, 512>(a, grid, st);
+  return tpr == 64    ? launch_norm_p<float, BWD, 64>(a, grid, st)
+         : tpr == 256 ? launch_norm_p<float, BWD, 256>(a, grid, st)
+                      : launch_norm_p<float, BWD, 512>(a, grid, st);
 }
 
 // Workgroups per group of rows, each of at least one turn of rows. The forward takes many short ones (16 per CU of
