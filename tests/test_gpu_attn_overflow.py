@@ -24,3 +24,16 @@ def test_keys_that_are_not_there_get_zero_beside_a_gradient_that_overflows(Nq, N
     _, dk, dv = R.rola_attn_backward(q, k, v, o, lse, do, kv_len=kv_len)
     assert bool(dv[:, :, 0].isinf().all())
     assert bool((dk[:, :, 1:] == 0).all()) and bool((dv[:, :, 1:] == 0).all())
+
+
+@pytest.mark.parametrize("power", [-60, 40, 90])
+@pytest.mark.parametrize("Nq,Nk", [(64, 40), (1500, 3000)])
+def test_bf16_gradients_scale_exactly_with_the_output_gradient(Nq, Nk, power):
+    """dO times a power of two, up to gradients of some 2^100: every bit of the gradients moves with it."""
+    g = torch.Generator(device="cuda").manual_seed(Nq)
+    q, k, v, do = (torch.randn((1, 2, n, 128), generator=g, device="cuda").to(torch.bfloat16) for n in (Nq, Nk, Nk, Nq))
+    o, lse = R.rola_attn(q, k, v, causal=True)
+    want = R.rola_attn_backward(q, k, v, o, lse, do, causal=True)
+    got = R.rola_attn_backward(q, k, v, o, lse, do * 2.0 ** power, causal=True)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b * 2.0 ** power)
