@@ -466,7 +466,7 @@ rola_status rola_attn(const rola_attn_problem* p, const rola_heads* Q, const rol
 /* Gradients of <dO, O> from O and lse of the forward (same kv_len, scale and mask), the probabilities
  * recomputed: dQ, dK, dV in dtype, summed in fp32 in a fixed order and rounded once. Keys behind a sample's
  * last get zero; key heads shared by several query heads get the sum over them. Q and dO must be finite, also
- * of a query that sees no key. */
+ * of a query that sees no key. bf16: dK and dV beyond 2^112 come out infinite. */
 size_t rola_attn_backward_workspace_bytes(const rola_attn_problem* p);
 rola_status rola_attn_backward(const rola_attn_problem* p, const rola_heads* Q, const rola_heads* K,
                                const rola_heads* V, const int32_t* kv_len, float softmax_scale,

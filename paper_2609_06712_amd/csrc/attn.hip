@@ -489,8 +489,7 @@ struct FwdPlan {
 };
 FwdPlan fwd_plan(const AttnShape& s) {
   const int R = s.Nq * (s.H / s.Hkv), bh = s.B * s.Hkv, steps = (s.Nk + 31) / 32;
-  // few rows. bf16: bound by reading K and V, in parts of a quarter round, which also evens out samples of
-  // different lengths; fp32: by latency
+  // few rows. bf16: bound by reading K and V, in parts of a quarter round; fp32: by latency
   const bool few = s.bf16 ? R <= 32 : f32_few((R + 63) / 64, bh) && (s.d == 64 || attn_work(s) < kFewForward);
   const int rows = few ? (s.bf16 ? 32 : 16) : s.bf16 ? 128 : 64, tiles = (R + rows - 1) / rows;
   const double bytes = rows * (s.d + 2) * 4.0;

@@ -33,7 +33,8 @@ constexpr int kTile = kRows * 256;   // its bytes (bf16, d 128)
 // of 65504) and is rounded by half a step of fp16 from 2^-29 on. Without it P below 2^-25 gave dK = 0, dK of 300000
 // keys was off by 0.0039 of its norm (0.0024), and single keys beside one that takes 0.999 of 8400 by up to 0.064 of
 // theirs (0.0049). The factor is a power of two, so no other rounding changes but that of lse - 15, 2^-21 at most below
-// an lse of 31. The times do not change.
+// an lse of 31; the times do not change. dK and dV are summed at 2^15 times their size, so what exceeds 2^112 comes out
+// infinite.
 constexpr float kLift = 15.f, kDrop = 1.f / 32768;
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));

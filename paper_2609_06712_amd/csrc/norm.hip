@@ -9,7 +9,7 @@
 // and a sum of squares about the wave's own mean each (their squares about the row's mean follow from the two).
 // A workgroup walks consecutive rows with its columns of W and b (and the gradient sums) in registers; the
 // next row's loads are under way during a row. All sums are fp32. Measured in a kernel trace, bf16: forward
-// 75600 x 5120 315 us (4.9 TB/s), 65520 x 1536 72 us and its backward 130 us (4.7 TB/s). The figures at the choices
+// 75600 x 5120 315 us (4.9 TB/s), 65520 x 1536 73 us and its backward 128 us (4.7 TB/s). The figures at the choices
 // below compare two forms at one time; a form that was made faster later takes less than they say.
 #include "common.h"
 #include "launch.h"
@@ -315,7 +315,8 @@ __global__ __launch_bounds__(norm_threads<TPR>()) void norm_bwd_kernel(const Nor
 // Threads per row. Up to 2048 channels a wave, which has no meeting with others per row (forward, 65520 rows of
 // 1536: 85 us, 100 with 256 threads; backward 147 and 156); for few rows 256, whose chain of loads and sums is a
 // quarter as long. Beyond, 256 or 512: forward 75600 x 5120 314 us with 256, 390 with 512, backward 499
-// and 487; 8192 x 8192 backward 103 and 100.
+// and 487; 8192 x 8192 backward 103 and 100. Rows of fewer than 512 channels leave lanes of their wave idle: 96 x 2^20
+// bf16 values as rows of 512, 256, 128, 64 channels take 82, 96, 176, 336 us forward and 136, 195, 327, 562 backward.
 int norm_row_threads(long rows, int d, bool bwd) {
   if (d > 8192) return 512;
   if (d > 2048) return bwd ? 512 : 256;
