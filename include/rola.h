@@ -439,10 +439,10 @@ rola_status rola_norm_backward(const rola_norm_problem* p, const void* X, int64_
  * h / (H / Hkv). Sample b has n = kv_len[b] keys (int32 [B], taken into [0, Nk]; NULL: all Nk); with
  * causal, query i sees keys j <= i + n - Nq (the last query sees all n). A query that sees no key has
  * O = 0 and lse = -inf. What lies behind a sample's keys is never used, whatever it holds; a key that the
- * causal mask hides from a query must still be finite. A query with a NaN or +inf score has O and lse NaN, and so
- * are the gradients that it has part in; other queries are as without it. lse (fp32 [B, H, Nq], may be NULL for
- * the forward) is log2 of the softmax denominator of the log2e-scaled scores: P = exp2(S log2e - lse),
- * S = scale Q K^T, as in rola_sparse_attn_lse.
+ * causal mask hides from a query must still be finite. A query with a NaN or +inf score has O, lse and dQ NaN, and so
+ * have the keys that it sees their dK and dV (those that the causal mask hides from it may have, too); other
+ * queries are as without it. lse (fp32 [B, H, Nq], may be NULL for the forward) is log2 of the softmax
+ * denominator of the log2e-scaled scores: P = exp2(S log2e - lse), S = scale Q K^T, as in rola_sparse_attn_lse.
  * Built for bf16 with d_h = 128 and fp32 with d_h 64 or 128; B H Nq, B Hkv Nk below 2^31, the stride
  * of the tokens below 2^26 bytes. */
 typedef struct rola_attn_problem {
